@@ -24,6 +24,7 @@ FB_DERR_NONE = 0
 FB_DERR_STATE = 1
 FB_DERR_PAGE = 2
 FB_DERR_PLAN = 3
+FB_DERR_RULE = 4
 
 FB_F32 = 0
 FB_BF16 = 1
@@ -34,6 +35,7 @@ FB_FORCE_PROGRESS = 2
 FB_SYNC_WINDOW = 4
 
 LAYOUTS = {"ragged": FB_RAGGED, "padded": FB_PADDED}
+GATES = {"none": 0, "all": 1, "request": 2, "row": 3}
 
 # Every symbol include/*.h declares.
 EXPORTS = [
@@ -46,6 +48,8 @@ EXPORTS = [
     "fb_synth_embed", "fb_synth_logits", "fb_decode_loop",
     "fb_lmhead_workspace_bytes", "fb_lmhead_reduce", "fb_window_prologue",
     "fb_hbm_read_probe", "fb_hbm_copy_probe", "fb_denoise_update_noalloc",
+    "fb_residual_norm", "fb_mx4_linear", "fb_rules_workspace_bytes", "fb_rules_build",
+    "fb_vocab_reduce_rules", "fb_logits_rules",
 ]
 FB_NOALLOC_SCRATCH_BYTES = 4 << 20
 FB_PROBE_BLOCKS = 2048
@@ -103,6 +107,18 @@ class fb_loop_args(ctypes.Structure):
         ("v_new", vp), ("k_cache", vp), ("v_cache", vp), ("page_table", vp),
         ("attn_out", vp), ("attn_ws", vp), ("attn_ws_bytes", sz),
         ("embed_seed", ctypes.c_uint64), ("counters", vp), ("forwards", vp)]
+
+
+class fb_norm_shape(ctypes.Structure):
+    _fields_ = [("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("gate", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("res_scale", ctypes.c_float), ("reserved", ctypes.c_int32 * 3)]
+
+
+class fb_logit_rules(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ("params", "bias_start", "bias_id", "bias_val", "masks", "row_mask")] + \
+        [("n_bias", ctypes.c_int32), ("n_masks", ctypes.c_int32)]
 
 
 # numpy views of the device records
@@ -168,6 +184,16 @@ def lib():
                                                 vp, i32, P(fb_pack), P(fb_update_params),
                                                 vp, vp]),
             "fb_hbm_copy_probe": (i32, [vp, vp, sz, vp]),
+            "fb_residual_norm": (i32, [vp, vp, vp, vp, vp, vp, vp, P(fb_pack),
+                                       P(fb_norm_shape), vp]),
+            "fb_mx4_linear": (i32, [vp, vp, vp, i32, i32, P(fb_pack), vp, i32, vp]),
+            "fb_rules_workspace_bytes": (sz, [P(fb_pack), i32]),
+            "fb_rules_build": (i32, [P(fb_logit_rules), vp, vp, i32, i32, P(fb_pack), vp,
+                                     sz, vp]),
+            "fb_vocab_reduce_rules": (i32, [vp, i32, i32, P(fb_pack), P(fb_logit_rules), vp,
+                                            sz, vp, sz, vp, vp, vp]),
+            "fb_logits_rules": (i32, [vp, vp, i32, i32, P(fb_pack), P(fb_logit_rules), vp, sz,
+                                      vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -418,6 +444,69 @@ def fb_lmhead_reduce(hidden, weight, pack, lm_ws, upd_ws, stream=None):
 def stats_to_numpy(stats_tensor, B):
     raw = stats_tensor.cpu().numpy().view(np.uint8)[: B * REQ_STATS_DTYPE.itemsize]
     return raw.view(REQ_STATS_DTYPE)
+
+
+# ------------------------------------------------------- the model's tail
+def make_norm_shape(D, dtype, gate="none", eps=1e-6, res_scale=1.0):
+    if not isinstance(dtype, int):
+        dtype = FB_BF16 if str(dtype) in ("bf16", "torch.bfloat16") else FB_F32
+    return fb_norm_shape(D, dtype, GATES[gate] if isinstance(gate, str) else gate, eps,
+                         res_scale)
+
+
+def fb_residual_norm(y, h, gate, w_post, w_pre, h_out, n_out, pack, shape, stream=None):
+    """u = rms(y) w_post, h_out = h + a g u, n_out = rms(h_out) w_pre on the live
+    rows; any of y, gate, w_post, w_pre, h_out, n_out may be None as the header says."""
+    _check(lib().fb_residual_norm(_ptr(y), _ptr(h), _ptr(gate), _ptr(w_post), _ptr(w_pre),
+                                  _ptr(h_out), _ptr(n_out), pack.ref(), ctypes.byref(shape),
+                                  _stream(stream)))
+
+
+def fb_mx4_linear(x, codes, scales, pack, y, stream=None):
+    """x bf16 [row_cap, K]; codes uint8 [N, K/2] (E2M1, element 2i in the low half
+    of byte i); scales uint8 [N, K/32] (E8M0); y [row_cap, N], bf16 or fp32."""
+    _check(lib().fb_mx4_linear(_ptr(x), _ptr(codes), _ptr(scales), codes.shape[0],
+                               x.shape[-1], pack.ref(), _ptr(y), _dtype_code(y),
+                               _stream(stream)))
+
+
+def make_rules(params=None, bias_start=None, bias_id=None, bias_val=None, masks=None,
+               row_mask=None):
+    """params fp32 [B, 4] (repetition, presence, frequency, 0); bias_start int32
+    [B+1] with bias_id int32 and bias_val fp32; masks int32 [n_masks,
+    ceil(V/32)] with row_mask int32 [row_cap].  Keeps its tensors alive."""
+    r = fb_logit_rules(_ptr(params), _ptr(bias_start), _ptr(bias_id), _ptr(bias_val),
+                       _ptr(masks), _ptr(row_mask), 0 if bias_id is None else bias_id.numel(),
+                       0 if masks is None else masks.shape[0])
+    r.tensors = (params, bias_start, bias_id, bias_val, masks, row_mask)
+    return r
+
+
+def fb_rules_workspace_bytes(pack, V):
+    return int(lib().fb_rules_workspace_bytes(pack.ref(), V))
+
+
+def fb_rules_build(rules, st, tokens, V, pack, ws, stream=None):
+    _check(lib().fb_rules_build(ctypes.byref(rules), _ptr(st), _ptr(tokens), tokens.shape[-1], V,
+                                pack.ref(), _ptr(ws), ws.numel() * ws.element_size(),
+                                _stream(stream)))
+
+
+def fb_vocab_reduce_rules(logits, pack, rules, rules_ws, upd_ws, conf=None, argmax=None,
+                          stream=None):
+    """The reduction under the rules lands in upd_ws for fb_denoise_apply, and, if
+    given, in conf fp32 and argmax int32 [row_cap]."""
+    _check(lib().fb_vocab_reduce_rules(_ptr(logits), logits.shape[-1], _dtype_code(logits),
+                                       pack.ref(), ctypes.byref(rules), _ptr(rules_ws),
+                                       rules_ws.numel() * rules_ws.element_size(), _ptr(upd_ws),
+                                       upd_ws.numel() * upd_ws.element_size(), _ptr(conf),
+                                       _ptr(argmax), _stream(stream)))
+
+
+def fb_logits_rules(logits, out, pack, rules, rules_ws, stream=None):
+    _check(lib().fb_logits_rules(_ptr(logits), _ptr(out), logits.shape[-1], _dtype_code(logits),
+                                 pack.ref(), ctypes.byref(rules), _ptr(rules_ws),
+                                 rules_ws.numel() * rules_ws.element_size(), _stream(stream)))
 
 
 # ------------------------------------------------------ multi-step loop

@@ -494,6 +494,176 @@ int fb_denoise_update_noalloc(const void* logits, int V, int dtype, int32_t* tok
     return ok();
 }
 
+// ---- the model's tail (flowblock_tail.h) ----------------------------------
+
+namespace {
+
+static bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+static bool overlap(const void* p, size_t np, const void* q, size_t nq) {
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+    return p && q && a < b + nq && b < a + np;
+}
+
+static int check_rules(const fb_logit_rules* r) {
+    if (!r) return fail(FB_E_INVAL, "rules is NULL");
+    if (r->n_bias < 0 || r->n_masks < 0)
+        return fail(FB_E_INVAL, "n_bias and n_masks must be >= 0");
+    if (r->bias_start && r->n_bias > 0 && (!r->bias_id || !r->bias_val))
+        return fail(FB_E_INVAL, "bias_start without bias_id or bias_val");
+    if (!r->masks != !r->row_mask) return fail(FB_E_INVAL, "masks and row_mask go together");
+    if (r->masks && r->n_masks < 1) return fail(FB_E_INVAL, "masks with n_masks %d", r->n_masks);
+    if (!aligned(r->params, 4) || !aligned(r->bias_start, 4) || !aligned(r->bias_id, 4) ||
+        !aligned(r->bias_val, 4) || !aligned(r->masks, 4) || !aligned(r->row_mask, 4))
+        return fail(FB_E_INVAL, "the rules' arrays must be 4-byte aligned");
+    return FB_OK;
+}
+
+static int check_rules_size(const fb_pack* pack, int V) {
+    int rc = check_pack(pack);
+    if (rc) return rc;
+    if (V < 1) return fail(FB_E_INVAL, "V must be >= 1");
+    if (V > (1 << 20)) return fail(FB_E_UNSUPPORTED, "V %d above 2^20", V);
+    return FB_OK;
+}
+
+static int check_rules_ws(const void* ws, size_t ws_bytes, size_t need) {
+    if (ws_bytes < need || !ws)
+        return fail(FB_E_WORKSPACE, "rules workspace has %zu bytes, needs %zu", ws_bytes, need);
+    if (!aligned16(ws)) return fail(FB_E_INVAL, "workspace must be 16-byte aligned");
+    return FB_OK;
+}
+
+}  // namespace
+
+int fb_residual_norm(const void* y, const void* h, const void* gate, const void* w_post,
+                     const void* w_pre, void* h_out, void* n_out, const fb_pack* pack,
+                     const fb_norm_shape* sh, void* stream) {
+    int rc = check_pack(pack);
+    if (rc) return rc;
+    if (!sh) return fail(FB_E_INVAL, "shape is NULL");
+    if (sh->D < 1) return fail(FB_E_INVAL, "D must be >= 1");
+    if (sh->D > 16384) return fail(FB_E_UNSUPPORTED, "D %d above 16384", sh->D);
+    if (sh->dtype != FB_BF16 && sh->dtype != FB_F32)
+        return fail(FB_E_UNSUPPORTED, "dtype %d not supported", sh->dtype);
+    if (sh->gate < FB_GATE_NONE || sh->gate > FB_GATE_ROW)
+        return fail(FB_E_INVAL, "gate layout %d", sh->gate);
+    if (!(sh->eps > 0.f) || isinf(sh->eps)) return fail(FB_E_INVAL, "eps must be finite and > 0");
+    if (isnan(sh->res_scale) || isinf(sh->res_scale))
+        return fail(FB_E_INVAL, "res_scale is not finite");
+    if (!h) return fail(FB_E_INVAL, "h is NULL");
+    if ((sh->gate == FB_GATE_NONE) != !gate)
+        return fail(FB_E_INVAL, "gate and its layout do not agree");
+    if (!y && (gate || w_post || h_out))
+        return fail(FB_E_INVAL, "a plain norm (y NULL) has no gate, w_post or h_out");
+    if (y && !h_out) return fail(FB_E_INVAL, "h_out is NULL");
+    if (!n_out && (w_pre || !y)) return fail(FB_E_INVAL, "n_out is NULL");
+    const size_t elt = sh->dtype == FB_BF16 ? 2 : 4;
+    const void* all[] = {y, h, gate, w_post, w_pre, h_out, n_out};
+    for (const void* p : all)
+        if (!aligned(p, elt)) return fail(FB_E_INVAL, "a pointer is not aligned to its type");
+    const size_t nb = (size_t)pack->row_cap * sh->D * elt;
+    if (overlap(h_out, nb, n_out, nb) || (h_out != h && overlap(h_out, nb, h, nb)) ||
+        overlap(h_out, nb, y, nb) || (n_out != h && overlap(n_out, nb, h, nb)) ||
+        (n_out != y && overlap(n_out, nb, y, nb)))
+        return fail(FB_E_INVAL, "outputs overlap each other or an input");
+    hipError_t e = fb::launch_residual_norm(y, h, gate, w_post, w_pre, h_out, n_out, pack, sh,
+                                            (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "residual norm launch");
+    return ok();
+}
+
+int fb_mx4_linear(const void* x, const void* codes, const void* scales, int N, int K,
+                  const fb_pack* pack, void* y, int y_dtype, void* stream) {
+    int rc = check_pack(pack);
+    if (rc) return rc;
+    if (N < 1) return fail(FB_E_INVAL, "N must be >= 1");
+    if (K < 32 || K % 32) return fail(FB_E_INVAL, "K %d must be a positive multiple of 32", K);
+    if (K > 65536) return fail(FB_E_UNSUPPORTED, "K %d above 65536", K);
+    if (y_dtype != FB_BF16 && y_dtype != FB_F32)
+        return fail(FB_E_UNSUPPORTED, "dtype %d not supported", y_dtype);
+    if (!x || !codes || !scales || !y) return fail(FB_E_INVAL, "a tensor pointer is NULL");
+    if (!aligned16(x) || !aligned16(codes))
+        return fail(FB_E_INVAL, "x and codes must be 16-byte aligned");
+    const size_t elt = y_dtype == FB_BF16 ? 2 : 4;
+    if (!aligned(y, elt)) return fail(FB_E_INVAL, "y is not aligned to its type");
+    if (overlap(x, (size_t)pack->row_cap * K * 2, y, (size_t)pack->row_cap * N * elt))
+        return fail(FB_E_INVAL, "x and y overlap");
+    hipError_t e = fb::launch_mx4_linear(x, codes, scales, N, K, pack, y, y_dtype,
+                                         (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "4-bit linear launch");
+    return ok();
+}
+
+size_t fb_rules_workspace_bytes(const fb_pack* pack, int V) {
+    if (check_rules_size(pack, V)) return 0;
+    return fb::rules_sizes(pack, V).total;
+}
+
+int fb_rules_build(const fb_logit_rules* rules, const fb_req_state* st, const int32_t* tokens,
+                   int T_max, int V, const fb_pack* pack, void* ws, size_t ws_bytes,
+                   void* stream) {
+    int rc = check_rules_size(pack, V);
+    if (rc) return rc;
+    rc = check_rules(rules);
+    if (rc) return rc;
+    if (!st || !tokens) return fail(FB_E_INVAL, "state or tokens is NULL");
+    if (T_max < 1) return fail(FB_E_INVAL, "T_max must be >= 1");
+    const fb::RulesSizes z = fb::rules_sizes(pack, V);
+    rc = check_rules_ws(ws, ws_bytes, z.total);
+    if (rc) return rc;
+    hipError_t e = fb::launch_rules_build(rules, st, tokens, T_max, V, pack, ws, z,
+                                          (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "rules build launch");
+    return ok();
+}
+
+int fb_vocab_reduce_rules(const void* logits, int V, int dtype, const fb_pack* pack,
+                          const fb_logit_rules* rules, const void* rules_ws,
+                          size_t rules_ws_bytes, void* upd_ws, size_t upd_ws_bytes, float* conf,
+                          int32_t* argmax, void* stream) {
+    int rc = check_rules_size(pack, V);
+    if (rc) return rc;
+    rc = check_reduce_args(pack, logits, V, dtype);
+    if (rc) return rc;
+    rc = check_rules(rules);
+    if (rc) return rc;
+    if (!conf != !argmax) return fail(FB_E_INVAL, "conf and argmax go together");
+    const fb::RulesSizes z = fb::rules_sizes(pack, V);
+    rc = check_rules_ws(rules_ws, rules_ws_bytes, z.total);
+    if (rc) return rc;
+    const fb::UpdateSizes uz = fb::update_sizes(pack, V, cu_count());
+    rc = check_ws(upd_ws, upd_ws_bytes, uz.total);
+    if (rc) return rc;
+    hipError_t e = fb::launch_vocab_rules(logits, V, dtype, pack, rules, rules_ws, z, upd_ws, uz,
+                                          conf, argmax, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "vocab reduction under rules launch");
+    return ok();
+}
+
+int fb_logits_rules(const void* logits, void* out, int V, int dtype, const fb_pack* pack,
+                    const fb_logit_rules* rules, const void* rules_ws, size_t rules_ws_bytes,
+                    void* stream) {
+    int rc = check_rules_size(pack, V);
+    if (rc) return rc;
+    rc = check_reduce_args(pack, logits, V, dtype);
+    if (rc) return rc;
+    rc = check_rules(rules);
+    if (rc) return rc;
+    if (!out || !aligned16(out)) return fail(FB_E_INVAL, "out must be a 16-byte aligned pointer");
+    const size_t nb = (size_t)pack->row_cap * V * (dtype == FB_BF16 ? 2 : 4);
+    if (out != logits && overlap(logits, nb, out, nb))
+        return fail(FB_E_INVAL, "out overlaps logits without being it");
+    const fb::RulesSizes z = fb::rules_sizes(pack, V);
+    rc = check_rules_ws(rules_ws, rules_ws_bytes, z.total);
+    if (rc) return rc;
+    const fb::UpdateSizes uz = fb::update_sizes(pack, V, cu_count());
+    hipError_t e = fb::launch_logits_rules(logits, out, V, dtype, pack, rules, rules_ws, z, uz,
+                                           (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "logit rules launch");
+    return ok();
+}
+
 // ---- multi-step loop on the synthetic model (flowblock_loop.h) -----------
 
 namespace {

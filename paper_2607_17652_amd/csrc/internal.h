@@ -7,6 +7,7 @@
 
 #include "flowblock.h"
 #include "flowblock_loop.h"
+#include "flowblock_tail.h"
 
 namespace fb {
 
@@ -117,6 +118,31 @@ LmSizes lm_sizes(const fb_pack* pack, int V, int D, int cu_count);
 hipError_t launch_lmhead(const void* hidden, const void* weight, int D, int V,
                          const fb_pack* pack, void* lm_ws, const LmSizes& z, void* upd_ws,
                          const UpdateSizes& uz, hipStream_t stream);
+
+hipError_t launch_residual_norm(const void* y, const void* h, const void* gate,
+                                const void* w_post, const void* w_pre, void* h_out,
+                                void* n_out, const fb_pack* pack, const fb_norm_shape* sh,
+                                hipStream_t stream);
+hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scales, int N, int K,
+                             const fb_pack* pack, void* y, int y_dtype, hipStream_t stream);
+
+struct RulesSizes {
+    int words;       // bitmap words per request, a multiple of 4
+    size_t off_bits, off_count, off_bias, total;
+};
+RulesSizes rules_sizes(const fb_pack* pack, int V);
+hipError_t launch_rules_build(const fb_logit_rules* rules, const fb_req_state* st,
+                              const int32_t* tokens, int T_max, int V, const fb_pack* pack,
+                              void* ws, const RulesSizes& z, hipStream_t stream);
+// `conf` and `argmax` may be NULL (both): partials only
+hipError_t launch_vocab_rules(const void* logits, int V, int dtype, const fb_pack* pack,
+                              const fb_logit_rules* rules, const void* rules_ws,
+                              const RulesSizes& rz, void* upd_ws, const UpdateSizes& uz,
+                              float* conf, int32_t* argmax, hipStream_t stream);
+hipError_t launch_logits_rules(const void* logits, void* out, int V, int dtype,
+                               const fb_pack* pack, const fb_logit_rules* rules,
+                               const void* rules_ws, const RulesSizes& rz,
+                               const UpdateSizes& uz, hipStream_t stream);
 
 struct SynthSizes {
     int nsplit;      // vocabulary partitions per row of the logits fill

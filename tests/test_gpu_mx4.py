@@ -1,0 +1,124 @@
+"""fb_mx4_linear against the float64 product with the format's own values.
+
+Tolerance: products are exact, a sum of K float32 terms is within
+gamma_K sum |x w| (Higham, Sec. 3.1; gamma_K = K u / (1 - K u), u = 2^-24),
+then half a step of y's type."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tail
+from paper_2607_17652_amd import binding as fb
+from tail_harness import BATCHES, HALF_STEP, TORCH, Batch, f64
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(bt, N, K, seed=0, lo=118, hi=130):
+    rng = np.random.default_rng(seed)
+    codes = rng.integers(0, 256, size=(N, K // 2), dtype=np.uint8)
+    scales = rng.integers(lo, hi, size=(N, K // 32), dtype=np.uint8)
+    x = torch.from_numpy(rng.standard_normal((bt.row_cap, K))).to(torch.bfloat16)
+    return codes, scales, x
+
+
+def call(bt, codes, scales, x, out):
+    y = torch.full((bt.row_cap, codes.shape[0]), 5.0, dtype=TORCH[out], device="cuda")
+    fb.fb_mx4_linear(x.cuda(), torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(),
+                     bt.pack, y)
+    return y
+
+
+def check(bt, codes, scales, x, y, out):
+    live, K = bt.live, x.shape[1]
+    w = tail.mx4_weights(codes, scales)
+    xs = x.double().numpy()[live]
+    exact = xs @ w.T
+    gamma = K * 2.0 ** -24 / (1 - K * 2.0 ** -24)
+    tol = gamma * (np.abs(xs) @ np.abs(w).T) + HALF_STEP[out] * np.abs(exact)
+    assert np.all(np.abs(f64(y)[live] - exact) <= tol)
+    dead = np.setdiff1d(np.arange(bt.row_cap), live)
+    assert np.all(f64(y)[dead] == 5)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("N,K", [(1, 32), (15, 64), (16, 96), (17, 128), (33, 160), (100, 992),
+                                 (128, 1024), (1000, 2080), (257, 4096), (40, 16384)])
+@pytest.mark.parametrize("batch", ["token", "ragged", "padded", "window96"])
+def test_sizes(batch, N, K, out):
+    bt = Batch(**BATCHES[batch]).cuda()
+    case = inputs(bt, N, K, seed=N + K)
+    check(bt, *case, call(bt, *case, out), out)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 31, 33, 48, 63, 64, 65, 80, 127, 128, 129, 200, 300])
+@pytest.mark.parametrize("N,K", [(96, 256), (2000, 512)])
+def test_row_counts(rows, N, K):
+    bt = Batch(w=[1], o=[3], bl=rows, W_max=1).cuda()
+    case = inputs(bt, N, K, seed=rows)
+    check(bt, *case, call(bt, *case, "f32"), "f32")
+
+
+@pytest.mark.parametrize("layout", ["ragged", "padded"])
+def test_many_rows_some_live(layout):
+    bt = Batch(w=[4, 1, 2, 4, 1, 3, 1, 1, 2, 4], o=[32] * 10, bl=32, W_max=4, layout=layout,
+               inactive=(3,)).cuda()
+    case = inputs(bt, 700, 1056, seed=5)
+    check(bt, *case, call(bt, *case, "bf16"), "bf16")
+
+
+def test_nothing_live_writes_nothing():
+    bt = Batch(**BATCHES["nothing"]).cuda()
+    case = inputs(bt, 64, 64)
+    assert torch.all(call(bt, *case, "f32") == 5)
+
+
+def test_every_code_and_scale_is_exact():
+    """x picks out single weights: the sixteen codes under the scales 2..252."""
+    bt = Batch(w=[1], o=[3], bl=32, W_max=1).cuda()
+    scales = np.arange(2, 253, dtype=np.uint8)[:, None]
+    codes = np.tile((np.arange(0, 32, 2) % 16 | (np.arange(1, 33, 2) % 16) << 4).astype(np.uint8),
+                    (251, 1))
+    x = torch.eye(32).to(torch.bfloat16)
+    y = f64(call(bt, codes, scales, x, "f32"))
+    assert np.array_equal(y, tail.mx4_weights(codes, scales).T)
+
+
+def test_nan_scale_spoils_its_output_alone():
+    bt = Batch(**BATCHES["ragged"]).cuda()
+    codes, scales, x = inputs(bt, 40, 256, seed=9)
+    clean = f64(call(bt, codes, scales, x, "f32"))
+    scales[7, 3] = 255
+    y = f64(call(bt, codes, scales, x, "f32"))
+    assert np.isnan(y[bt.live, 7]).all()
+    others = np.arange(40) != 7
+    assert np.array_equal(y[:, others], clean[:, others])
+
+
+def test_rows_stand_alone():
+    """Infinities and NaN of one row, and dead rows' contents, reach no other
+    row; a row's result is the same bits beside any others."""
+    bt = Batch(**BATCHES["padded"]).cuda()
+    codes, scales, x = inputs(bt, 70, 320, seed=4)
+    clean = f64(call(bt, codes, scales, x, "f32"))
+    x2 = x.clone()
+    dead = np.setdiff1d(np.arange(bt.row_cap), bt.live)
+    x2[dead] = float("nan")
+    x2[bt.live[0]] = float("inf")
+    y = f64(call(bt, codes, scales, x2, "f32"))
+    assert np.array_equal(y[bt.live[1:]], clean[bt.live[1:]])
+
+
+def test_large_vocabulary():
+    """An LM head: sampled columns of 157184, one token and one window."""
+    N, K = 157184, 2048
+    g = torch.Generator(device="cuda").manual_seed(0)
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(118, 126, (N, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+    pick = np.r_[0:40, 78000:78040, N - 40:N]
+    for batch in ("token", "window96"):
+        bt = Batch(**BATCHES[batch]).cuda()
+        x = torch.randn(bt.row_cap, K, generator=g, device="cuda").to(torch.bfloat16)
+        y = torch.full((bt.row_cap, N), 5.0, device="cuda")
+        fb.fb_mx4_linear(x, codes, scales, bt.pack, y)
+        check(bt, codes[pick].cpu().numpy(), scales[pick].cpu().numpy(), x.cpu(), y[:, pick], "f32")
