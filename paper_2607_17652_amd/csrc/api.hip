@@ -589,7 +589,7 @@ int fb_mx4_linear(const void* x, const void* codes, const void* scales, int N, i
     if (!aligned(y, elt)) return fail(FB_E_INVAL, "y is not aligned to its type");
     if (overlap(x, (size_t)pack->row_cap * K * 2, y, (size_t)pack->row_cap * N * elt))
         return fail(FB_E_INVAL, "x and y overlap");
-    hipError_t e = fb::launch_mx4_linear(x, codes, scales, N, K, pack, y, y_dtype,
+    hipError_t e = fb::launch_mx4_linear(x, codes, scales, N, K, pack, y, y_dtype, cu_count(),
                                          (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "4-bit linear launch");
     return ok();

@@ -124,7 +124,8 @@ hipError_t launch_residual_norm(const void* y, const void* h, const void* gate,
                                 void* n_out, const fb_pack* pack, const fb_norm_shape* sh,
                                 hipStream_t stream);
 hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scales, int N, int K,
-                             const fb_pack* pack, void* y, int y_dtype, hipStream_t stream);
+                             const fb_pack* pack, void* y, int y_dtype, int cu_count,
+                             hipStream_t stream);
 
 struct RulesSizes {
     int words;       // bitmap words per request, a multiple of 4

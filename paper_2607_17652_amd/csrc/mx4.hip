@@ -1,88 +1,292 @@
 // Linear layers with MXFP4 weights on the packed live rows: y = W x, W's
 // element 2^(scale - 127) E2M1(code), one scale per 32 of K.
 //
-// mx4_kernel  one wave per output column; lanes along K.
+// An E2M1 value has two significant bits and the scale is a power of two, so
+// v_cvt_scalef32_pk_bf16_fp4 turns two codes and their scale into two bf16
+// weights exactly, and the products run on v_mfma_f32_16x16x32_bf16: A holds
+// 16 columns of the output (rows of W), B 16 tokens, and a lane's result is
+// four neighbouring columns of one token.  A dot product does not care which k
+// goes into which slot, so lane group g (of four) of a 128-wide chunk of K
+// takes the 32 elements k = 32 g ..: one 16-byte read of codes, one scale.
+//
+// mx4_kernel  a workgroup of eight waves walks K in chunks through a ring of
+//             LDS stages, filled by direct global->LDS loads: x (shared by the
+//             waves), and each wave's own codes and scales.  A wave owns NT
+//             16-column tiles; where the columns are few, KW waves share a
+//             tile, take the chunks of a stage in turn and join at the end.
+#include <type_traits>
+
 #include "internal.h"
 
 namespace fb {
 namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kMxThreads = 256;
-constexpr int kMxRows = 8;
+constexpr int kWaves = 8;
+constexpr int kMxThreads = kWaves * 64;
+constexpr int kLdsBytes = 160 * 1024;
 
-// Element pair j of a dword of codes, times 2^(scale-127): exact in bf16.
-template <int J>
-__device__ inline uint32_t weight_pair(uint32_t codes, float scale) {
-    const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, J);
-    return __builtin_bit_cast(uint32_t, p);
+// What stands in x past K.
+__device__ __attribute__((aligned(16))) uint32_t mx4_zeros[4] = {0, 0, 0, 0};
+
+struct MxArgs {
+    const uint16_t* x;
+    const uint8_t* codes;
+    const uint8_t* scales;
+    void* y;
+    int N, K, row_cap, bf16_out, vec_out;
+};
+
+// Eight weights (one dword of codes) as the MFMA's A operand; the scale is a
+// float whose exponent is the E8M0 code.
+__device__ inline bf16x8 weights8(uint32_t codes, float scale) {
+    union {
+        bf16x2 p[4];
+        bf16x8 v;
+    } w;
+    w.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+    w.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+    w.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+    w.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+    return w.v;
 }
 
-__device__ inline float lo_f(uint32_t p) { return __uint_as_float(p << 16); }
-__device__ inline float hi_f(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
-
-template <typename T>
-__global__ void __launch_bounds__(kMxThreads)
-mx4_kernel(const uint16_t* __restrict__ x, const uint8_t* __restrict__ codes,
-           const uint8_t* __restrict__ scales, int N, int K, PackView pv, int row_cap,
-           T* __restrict__ y) {
-    const int n = blockIdx.x * (kMxThreads / 64) + (threadIdx.x >> 6);
+// Bit i of the result: row r0 + i is live (i < 64 in m0, then m1).
+__device__ inline void live_rows(const PackView& pv, int r0, int row_cap, uint64_t& m0,
+                                 uint64_t& m1, int n) {
     const int lane = threadIdx.x & 63;
-    const int row0 = blockIdx.y * kMxRows;
-    if (n >= N) return;
-    bool live[kMxRows];
-    bool any = false;
+    const int r = r0 + lane;
+    m0 = __ballot(lane < n && r < row_cap && pv.row_req[min(r, row_cap - 1)] >= 0);
+    m1 = n > 64 ? __ballot(r + 64 < row_cap && pv.row_req[min(r + 64, row_cap - 1)] >= 0) : 0;
+}
+
+__device__ inline void store4(const MxArgs& a, int row, int n, const f32x4& v) {
+    const size_t at = (size_t)row * a.N + n;
+    if (a.bf16_out) {
+        uint16_t* p = static_cast<uint16_t*>(a.y) + at;
+        uint16_t h[4];
 #pragma unroll
-    for (int i = 0; i < kMxRows; ++i) {
-        live[i] = row0 + i < row_cap && pv.row_req[row0 + i] >= 0;
-        any |= live[i];
-    }
-    if (!any) return;
-    float acc[kMxRows] = {};
-    for (int g = lane; g < K / 32; g += 64) {
-        const uint4 c = *reinterpret_cast<const uint4*>(codes + (size_t)n * (K / 2) + g * 16);
-        const uint32_t e = scales[(size_t)n * (K / 32) + g];
-        const float s = e == 255 ? __uint_as_float(0x7fc00000u) : 1.f;
-        const float f = __uint_as_float(e << 23);
-        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-        uint32_t p[16];
+        for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+        if (a.vec_out && n < a.N) {
+            *reinterpret_cast<uint2*>(p) =
+                make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+        } else {
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            p[4 * d] = weight_pair<0>(w[d], f);
-            p[4 * d + 1] = weight_pair<1>(w[d], f);
-            p[4 * d + 2] = weight_pair<2>(w[d], f);
-            p[4 * d + 3] = weight_pair<3>(w[d], f);
+            for (int i = 0; i < 4; ++i)
+                if (n + i < a.N) p[i] = h[i];
         }
+    } else {
+        float* p = static_cast<float*>(a.y) + at;
+        if (a.vec_out && n < a.N) {
+            *reinterpret_cast<f32x4*>(p) = v;
+        } else {
 #pragma unroll
-        for (int i = 0; i < kMxRows; ++i) {
-            if (!live[i]) continue;
-            const uint4* xr = reinterpret_cast<const uint4*>(x + (size_t)(row0 + i) * K + g * 32);
+            for (int i = 0; i < 4; ++i)
+                if (n + i < a.N) p[i] = v[i];
+        }
+    }
+}
+
+
+// Direct global->LDS loads; lane l's 16 bytes land at lds + 16 l (its byte,
+// widened, at lds + 4 l).
+__device__ inline void dma16(uint32_t lds, uint32_t off, const void* base) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ inline void dma16(uint32_t lds, const void* p) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(lds), "v"(p) : "memory");
+}
+__device__ inline void dma1(uint32_t lds, uint32_t off, const void* base) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_ubyte %1, %2"
+                 :: "s"(lds), "v"(off), "s"(base) : "memory");
+}
+
+// TT 16-token tiles, NT 16-column tiles a wave, KW waves to a tile.
+template <int TT, int NT, int KW>
+struct MxShape {
+    static constexpr int kX = KW * TT * 4096;               // x of a stage
+    static constexpr int kW = NT * 1280;                    // a wave's codes and scales
+    static constexpr int kStage = kX + kWaves * kW;
+    static constexpr int kFit = kLdsBytes / kStage;
+    static constexpr int kStages = kFit > 4 ? 4 : kFit;
+    static constexpr int kXOps = KW * TT > 2 ? KW * TT / 2 : 1;   // x loads per wave and stage
+    static constexpr int kOps = kXOps + 2 * NT;
+    static_assert(kStages >= 2 && (kStages - 2) * kOps < 64 && (KW == 1 || NT == 1));
+    static_assert(KW == 1 || kWaves * TT * 1024 <= kStages * kStage);
+};
+
+template <int TT, int NT, int KW>
+__global__ void __launch_bounds__(kMxThreads)
+mx4_kernel(MxArgs a, PackView pv, int n_groups) {
+    using S = MxShape<TT, NT, KW>;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[S::kStages * S::kStage];
+    const int ng = blockIdx.x % n_groups;
+    const int r0 = blockIdx.x / n_groups * (TT * 16);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint64_t m0, m1;
+    live_rows(pv, r0, a.row_cap, m0, m1, TT * 16);
+    if (!(m0 | m1)) return;   // uniform over the workgroup
+
+    const int kq = wave % KW;
+    const int n0 = (ng * (kWaves / KW) + wave / KW) * (NT * 16);
+    const int lr = lane & 15, g = lane >> 4;
+    const int C = (a.K + 127) / 128;
+    const int steps = (C + KW - 1) / KW;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0];
+
+    // ---- loads ---------------------------------------------------------------
+    // codes: four neighbouring lanes take one row's 64 bytes of a chunk, the
+    // 16-byte pieces turned by row / 4 so that the 16 rows of a read cover all
+    // banks.  x: sixteen lanes take one row's 256 bytes, turned by the row.
+    const int wr = lane >> 2, wp = (lane & 3) ^ (wr >> 2);
+    const int nb = min(n0, a.N - 1);
+    const uint8_t* cbase = a.codes + (size_t)nb * (a.K / 2);
+    const uint8_t* sbase = a.scales + (size_t)nb * (a.K / 32);
+    int nrow[NT];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint4 xv = xr[q];
-                const uint32_t xs[4] = {xv.x, xv.y, xv.z, xv.w};
+    for (int n = 0; n < NT; ++n) nrow[n] = min(n * 16 + wr, a.N - 1 - nb);
+    const uint16_t* xbase = a.x + (size_t)r0 * a.K;
+    uint32_t x_off[S::kXOps];
+    int x_cc[S::kXOps];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    acc[i] = fmaf(lo_f(xs[j]), s * lo_f(p[4 * q + j]), acc[i]);
-                    acc[i] = fmaf(hi_f(xs[j]), s * hi_f(p[4 * q + j]), acc[i]);
+    for (int i = 0; i < S::kXOps; ++i) {
+        const int o = (wave * S::kXOps + i) % (KW * TT * 4);
+        const int r = (o % (TT * 4)) * 4 + (lane >> 4);
+        x_cc[i] = o / (TT * 4);
+        x_off[i] = (uint32_t)min(r, a.row_cap - 1 - r0) * (uint32_t)a.K * 2 +
+                   ((lane & 15) ^ (r & 15)) * 16;
+    }
+    auto issue = [&](int s, int slot) {
+        const uint32_t at = lds0 + slot * S::kStage;
+#pragma unroll
+        for (int i = 0; i < S::kXOps; ++i) {
+            const int o = (wave * S::kXOps + i) % (KW * TT * 4);
+            const int c = min(s * KW + x_cc[i], C - 1);
+            if (c * 128 + 128 <= a.K) {
+                dma16(at + o * 1024, x_off[i], xbase + c * 128);
+            } else {
+                const int r = (o % (TT * 4)) * 4 + (lane >> 4);
+                const int k = c * 128 + ((lane & 15) ^ (r & 15)) * 8;
+                const void* p = k < a.K
+                    ? static_cast<const void*>(reinterpret_cast<const char*>(xbase + c * 128) + x_off[i])
+                    : static_cast<const void*>(mx4_zeros);
+                dma16(at + o * 1024, p);
+            }
+        }
+        const int c = min(s * KW + kq, C - 1);
+        // a group past K reads the chunk's first one in its place
+        const int piece = (4 * c + wp) * 32 < a.K ? wp : 0;
+        const int byte = (4 * c + (lane & 3)) * 32 < a.K ? (lane & 3) : 0;
+        const uint32_t mine = at + S::kX + wave * S::kW;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            dma16(mine + n * 1024, (uint32_t)nrow[n] * (uint32_t)(a.K / 2) + piece * 16,
+                  cbase + c * 64);
+            dma1(mine + NT * 1024 + n * 256, (uint32_t)nrow[n] * (uint32_t)(a.K / 32) + byte,
+                 sbase + c * 4);
+        }
+    };
+
+    f32x4 acc[TT][NT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    bool nan[NT] = {};
+    const bool idle = n0 >= a.N;
+
+    // One barrier a stage: behind it stage s has landed for every wave, and
+    // the slot that stage s - 1 was read from is free.
+#pragma unroll
+    for (int s = 0; s < S::kStages - 1; ++s)
+        if (s < steps) issue(s, s);
+    int slot = 0;
+    for (int s = 0; s < steps; ++s) {
+        if (s + S::kStages - 2 < steps) {
+            asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S::kStages - 2) * S::kOps) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (s + S::kStages - 1 < steps)
+            issue(s + S::kStages - 1, slot == 0 ? S::kStages - 1 : slot - 1);
+        const int c = s * KW + kq;
+        if (c < C && !idle) {
+            const unsigned char* xs = lds + slot * S::kStage + kq * (TT * 4096);
+            const unsigned char* ws = lds + slot * S::kStage + S::kX + wave * S::kW;
+            u32x4 q[NT];
+            float sc[NT];
+            const bool some = (4 * c + g) * 32 < a.K;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                q[n] = *reinterpret_cast<const u32x4*>(ws + n * 1024 + lr * 64 + (g ^ (lr >> 2)) * 16);
+                uint32_t e = *reinterpret_cast<const uint32_t*>(ws + NT * 1024 + n * 256 + lr * 16 + g * 4);
+                e = some ? e & 255 : 0;
+                nan[n] |= e == 255;
+                sc[n] = __uint_as_float(e << 23);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bf16x8 w[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) w[n] = weights8(q[n][j], sc[n]);
+#pragma unroll
+                for (int t = 0; t < TT; ++t) {
+                    const bf16x8 b = *reinterpret_cast<const bf16x8*>(
+                        xs + (t * 16 + lr) * 256 + ((g * 4 + j) ^ lr) * 16);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], b, acc[t][n], 0, 0, 0);
                 }
             }
         }
+        slot = slot == S::kStages - 1 ? 0 : slot + 1;
     }
+
+    // a NaN scale makes its column NaN
 #pragma unroll
-    for (int i = 0; i < kMxRows; ++i) {
-        float v = acc[i];
+    for (int n = 0; n < NT; ++n) {
+        uint64_t m = __ballot(nan[n]);
+        if (m) {
+            m |= m >> 32;
+            m |= m >> 16;
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-        if (lane == 0 && live[i]) {
-            T* out = y + (size_t)(row0 + i) * N + n;
-            if constexpr (sizeof(T) == 2) {
-                const __bf16 r = (__bf16)v;
-                *out = __builtin_bit_cast(uint16_t, r);
-            } else {
-                *out = v;
-            }
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (m >> (4 * g + i) & 1) acc[t][n][i] = __uint_as_float(0x7fc00000u);
+        }
+    }
+    if constexpr (KW == 1) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const uint64_t m = t < 4 ? m0 >> (16 * t) : m1 >> (16 * (t - 4));
+            if (!(m >> lr & 1)) continue;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                store4(a, r0 + t * 16 + lr, n0 + n * 16 + g * 4, acc[t][n]);
+        }
+    } else {
+        // the KW waves of a tile share its token tiles; partials added in order
+        f32x4* part = reinterpret_cast<f32x4*>(lds);
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TT; ++t) part[(wave * TT + t) * 64 + lane] = acc[t][0];
+        __syncthreads();
+        for (int t = kq; t < TT; t += KW) {
+            const f32x4* p = part + (wave - kq) * TT * 64 + t * 64 + lane;
+            f32x4 v = p[0];
+#pragma unroll
+            for (int w = 1; w < KW; ++w) v += p[w * TT * 64];
+            const uint64_t m = t < 4 ? m0 >> (16 * t) : m1 >> (16 * (t - 4));
+            if (m >> lr & 1) store4(a, r0 + t * 16 + lr, n0 + g * 4, v);
         }
     }
 }
@@ -90,18 +294,64 @@ mx4_kernel(const uint16_t* __restrict__ x, const uint8_t* __restrict__ codes,
 }  // namespace
 
 hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scales, int N, int K,
-                             const fb_pack* pack, void* y, int y_dtype, hipStream_t stream) {
+                             const fb_pack* pack, void* y, int y_dtype, int cu_count,
+                             hipStream_t stream) {
     PackView pv = pack_view(pack);
-    const dim3 grid((N + 3) / 4, (pack->row_cap + kMxRows - 1) / kMxRows);
-    auto go = [&](auto zero) {
-        using T = decltype(zero);
-        hipLaunchKernelGGL(mx4_kernel<T>, grid, dim3(kMxThreads), 0, stream,
-                           static_cast<const uint16_t*>(x), static_cast<const uint8_t*>(codes),
-                           static_cast<const uint8_t*>(scales), N, K, pv, pack->row_cap,
-                           static_cast<T*>(y));
+    const int cap = pack->row_cap;
+    MxArgs a{static_cast<const uint16_t*>(x), static_cast<const uint8_t*>(codes),
+             static_cast<const uint8_t*>(scales), y, N, K, cap, y_dtype == FB_BF16 ? 1 : 0, 0};
+    a.vec_out = N % 4 == 0 && ((uintptr_t)y & (y_dtype == FB_BF16 ? 7 : 15)) == 0;
+    const int tiles = (N + 15) / 16;
+    auto launch = [&](auto tt, auto nt, auto kw) {
+        constexpr int T = decltype(tt)::value, M = decltype(nt)::value, W = decltype(kw)::value;
+        const int per = kWaves / W * M;
+        const int groups = (tiles + per - 1) / per;
+        const int rg = (cap + T * 16 - 1) / (T * 16);
+        hipLaunchKernelGGL((mx4_kernel<T, M, W>), dim3((unsigned)groups * rg), dim3(kMxThreads), 0,
+                           stream, a, pv, groups);
     };
-    if (y_dtype == FB_BF16) go(uint16_t());
-    else go(float());
+    using std::integral_constant;
+#define FB_C(n) integral_constant<int, n>()
+    const int rows16 = (cap + 15) / 16;
+    // few columns: split K until every CU has a workgroup
+    const int TT = rows16 <= 1 ? 1 : rows16 <= 2 ? 2 : rows16 <= 4 ? 4 : rows16 <= 6 ? 6 : 8;
+    auto units = [&](int tt) { return (long long)tiles * ((rows16 + tt - 1) / tt); };
+    const long long want = 8LL * cu_count;     // one tile per wave
+    if (units(TT) <= want / 2) {
+        const int t = TT > 4 ? 4 : TT;
+        if (units(t) <= want / 8 && t == 1) launch(FB_C(1), FB_C(1), FB_C(8));
+        else if (units(t) <= want / 8 && t == 2) launch(FB_C(2), FB_C(1), FB_C(8));
+        else if (units(t) <= want / 4 || t < 4) {
+            if (t == 1) launch(FB_C(1), FB_C(1), FB_C(4));
+            else if (t == 2) launch(FB_C(2), FB_C(1), FB_C(4));
+            else launch(FB_C(4), FB_C(1), FB_C(4));
+        } else launch(FB_C(4), FB_C(1), FB_C(2));
+        return hipGetLastError();
+    }
+    // tiles per wave: the least (rounds of workgroups) x (tiles + a start)
+    int nt = 1;
+    double best = 1e30;
+    for (int n = 1; n <= (TT == 8 ? 4 : 5); ++n) {
+        const long long groups = (tiles + 8 * n - 1) / (8 * n) * ((rows16 + TT - 1) / TT);
+        const double cost = (double)((groups + cu_count - 1) / cu_count) * (n + 0.5);
+        if (cost < best) {
+            best = cost;
+            nt = n;
+        }
+    }
+    auto pick = [&](auto tt) {
+        if (nt == 1) launch(tt, FB_C(1), FB_C(1));
+        else if (nt == 2) launch(tt, FB_C(2), FB_C(1));
+        else if (nt == 3) launch(tt, FB_C(3), FB_C(1));
+        else if (nt == 4) launch(tt, FB_C(4), FB_C(1));
+        else if constexpr (decltype(tt)::value < 8) launch(tt, FB_C(5), FB_C(1));
+    };
+    if (TT == 1) pick(FB_C(1));
+    else if (TT == 2) pick(FB_C(2));
+    else if (TT == 4) pick(FB_C(4));
+    else if (TT == 6) pick(FB_C(6));
+    else pick(FB_C(8));
+#undef FB_C
     return hipGetLastError();
 }
 
