@@ -568,7 +568,7 @@ int fb_residual_norm(const void* y, const void* h, const void* gate, const void*
         (n_out != y && overlap(n_out, nb, y, nb)))
         return fail(FB_E_INVAL, "outputs overlap each other or an input");
     hipError_t e = fb::launch_residual_norm(y, h, gate, w_post, w_pre, h_out, n_out, pack, sh,
-                                            (hipStream_t)stream);
+                                            cu_count(), (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "residual norm launch");
     return ok();
 }

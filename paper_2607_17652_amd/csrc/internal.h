@@ -122,7 +122,7 @@ hipError_t launch_lmhead(const void* hidden, const void* weight, int D, int V,
 hipError_t launch_residual_norm(const void* y, const void* h, const void* gate,
                                 const void* w_post, const void* w_pre, void* h_out,
                                 void* n_out, const fb_pack* pack, const fb_norm_shape* sh,
-                                hipStream_t stream);
+                                int cu_count, hipStream_t stream);
 hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scales, int N, int K,
                              const fb_pack* pack, void* y, int y_dtype, int cu_count,
                              hipStream_t stream);
