@@ -129,7 +129,7 @@ typedef struct fb_logit_rules {
 #define FB_DERR_RULE 4
 
 /* Workspace bytes of fb_rules_build for this pack and vocabulary, 0 if the
- * arguments are invalid.  V at most 2^20. */
+ * arguments are invalid.  V at most 2^19. */
 size_t fb_rules_workspace_bytes(const fb_pack* pack, int V);
 
 /* Writes into `ws` what the rules need of each request: which tokens are seen

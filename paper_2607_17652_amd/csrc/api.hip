@@ -523,7 +523,7 @@ static int check_rules_size(const fb_pack* pack, int V) {
     int rc = check_pack(pack);
     if (rc) return rc;
     if (V < 1) return fail(FB_E_INVAL, "V must be >= 1");
-    if (V > (1 << 20)) return fail(FB_E_UNSUPPORTED, "V %d above 2^20", V);
+    if (V > (1 << 19)) return fail(FB_E_UNSUPPORTED, "V %d above 2^19", V);
     return FB_OK;
 }
 
@@ -613,7 +613,7 @@ int fb_rules_build(const fb_logit_rules* rules, const fb_req_state* st, const in
     rc = check_rules_ws(ws, ws_bytes, z.total);
     if (rc) return rc;
     hipError_t e = fb::launch_rules_build(rules, st, tokens, T_max, V, pack, ws, z,
-                                          (hipStream_t)stream);
+                                          cu_count(), (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "rules build launch");
     return ok();
 }

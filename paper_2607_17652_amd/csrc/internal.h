@@ -129,12 +129,13 @@ hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scale
 
 struct RulesSizes {
     int words;       // bitmap words per request, a multiple of 4
-    size_t off_bits, off_count, off_bias, total;
+    int spans;       // lookups into its list of touched tokens
+    size_t off_bits, off_spans, off_adj, total;
 };
 RulesSizes rules_sizes(const fb_pack* pack, int V);
 hipError_t launch_rules_build(const fb_logit_rules* rules, const fb_req_state* st,
                               const int32_t* tokens, int T_max, int V, const fb_pack* pack,
-                              void* ws, const RulesSizes& z, hipStream_t stream);
+                              void* ws, const RulesSizes& z, int cu_count, hipStream_t stream);
 // `conf` and `argmax` may be NULL (both): partials only
 hipError_t launch_vocab_rules(const void* logits, int V, int dtype, const fb_pack* pack,
                               const fb_logit_rules* rules, const void* rules_ws,

@@ -1,17 +1,21 @@
 // Penalties for repeated tokens, biases and grammar masks on the live rows'
 // logits, in front of the denoise update's reduction.
 //
-// rules_build_kernel   one workgroup per request turns its committed prefix and
-//                      its biases into a bitmap of touched tokens and, at those
-//                      tokens only, a count word and a bias.  The dense arrays
-//                      are never cleared: an entry is read only where its bit
-//                      is set, and every such entry was written by this build.
-// vocab_rules_kernel   the vocabulary pass (the same pieces, folds and merges)
-//                      on adjusted logits; a group of logits costs one more
-//                      byte of bitmap and one of mask, and the gather of counts
-//                      and biases only where a bit is set.
+// rules_build_kernel   turns the committed prefix and the biases of a request
+//                      into a bitmap of touched tokens and a list, in token
+//                      order, of what is added to each.  A workgroup per slice
+//                      of the vocabulary: a slice's list has its own place, so
+//                      no workgroup waits for another.
+// vocab_rules_kernel   the vocabulary pass on adjusted logits.  A wave takes
+//                      windows of 4 KB: its logits fold as in the plain pass,
+//                      touched tokens left out; where the window has any, it is
+//                      also staged in LDS and its list entries are adjusted and
+//                      folded from there, one a lane.
 // predict_kernel       merges a row's partials into (p, x_hat).
-// logits_rules_kernel  the adjusted logits, written.
+// logits_rules_kernel  the adjusted logits, written: the list entries patch the
+//                      staged window, which is then stored.
+#include <type_traits>
+
 #include "internal.h"
 #include "vocab.h"
 
@@ -19,46 +23,94 @@ namespace fb {
 namespace {
 
 constexpr int kBuildThreads = 1024;
-constexpr uint32_t kSeen = 0x80000000u;   // count word: seen; the rest is c_v
+constexpr int kSpan = 1024;               // tokens whose list entries are found by one lookup
+constexpr int kSlice = 2 * kSpan;         // slices of the build are multiples of it
+constexpr uint32_t kSeen = 0x80000000u;   // beside a count or an id: the token is seen
 
+// What fb_rules_build leaves of request b:
+//   rec    repetition (NaN if the rules are unsound) and its reciprocal
+//   bits   the touched tokens (seen or biased), a bit each
+//   spans  per kSpan tokens, first and one past the last of their entries
+//   adj    per touched token what is added, and its id, kSeen set if it is seen;
+//          the entries of a slice lie together from its first token's place on
 struct RuleView {
-    float4* rec;          // [B] repetition, presence, frequency, 1 if sound
+    float2* rec;          // [B]
     uint32_t* bits;       // [B][words]
-    uint32_t* count;      // [B][words * 32]
-    float* bias;          // [B][words * 32]
-    int words;
+    uint2* spans;         // [B][spans]
+    uint2* adj;           // [B][words * 32]
+    int words, n_spans;
 };
 
 inline RuleView rule_view(const RulesSizes& z, void* ws) {
     char* p = static_cast<char*>(ws);
-    return RuleView{reinterpret_cast<float4*>(p), reinterpret_cast<uint32_t*>(p + z.off_bits),
-                    reinterpret_cast<uint32_t*>(p + z.off_count),
-                    reinterpret_cast<float*>(p + z.off_bias), z.words};
+    return RuleView{reinterpret_cast<float2*>(p), reinterpret_cast<uint32_t*>(p + z.off_bits),
+                    reinterpret_cast<uint2*>(p + z.off_spans),
+                    reinterpret_cast<uint2*>(p + z.off_adj), z.words, z.spans};
 }
 
 __device__ inline bool finite(float x) { return fabsf(x) < INFINITY; }
 
+// What is added to a touched token's logit: (bias - [c > 0] p) - f c.
+__device__ inline float addend(float bias, uint32_t c, const fb_rule_params& p) {
+#pragma clang fp contract(off)
+    const float a = bias - (c ? p.presence : 0.f);
+    const float b = p.frequency * (float)c;
+    return a - b;
+}
+
+// Barrier behind which the workgroup sees its own stores to memory, and its
+// atomics come after them.  (A device-wide fence would write the L2 back: the
+// build of 256 requests took 160 us with two of them, 12 with this.)
+__device__ inline void workgroup_sync() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// Calls f(i, token - v0) for the tokens of [0, n) that lie in [v0, v0 + nv), the
+// loads of eight rounds in flight together.
+template <typename F>
+__device__ inline void each_token(const int32_t* tok, int n, int v0, int nv, F&& f) {
+    constexpr int U = 8;
+    for (int i0 = threadIdx.x; i0 < n; i0 += U * kBuildThreads) {
+        int v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * kBuildThreads;
+            v[u] = i < n ? tok[i] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v[u] >= v0 && v[u] - v0 < nv) f(i0 + u * kBuildThreads, v[u] - v0);
+    }
+}
+
+// Workgroup (b, s): tokens [s * slice, (s + 1) * slice) of request b.  LDS: the
+// slice's bitmap, per word the touched tokens before it, and a count per touched
+// token (in adj where there are more than `lds_counts`).
 __global__ void __launch_bounds__(kBuildThreads)
 rules_build_kernel(fb_logit_rules rules, const fb_req_state* __restrict__ st,
                    const int32_t* __restrict__ tokens, int T_max, int V, PackView pv,
-                   RuleView rv) {
+                   RuleView rv, int slice, int n_slices, int lds_counts) {
     extern __shared__ uint32_t s_bits[];
+    const int b = blockIdx.x / n_slices;
+    const int v0 = blockIdx.x % n_slices * slice;
+    const int nv = min(slice, V - v0);
+    const int words = (nv + 31) / 32;
+    uint32_t* s_rank = s_bits + words;
+    uint32_t* s_count = s_rank + words;
     __shared__ int s_bad;
-    const int b = blockIdx.x;
-    const int tid = threadIdx.x;
+    __shared__ uint32_t s_wave[kBuildThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (pv.req_w[b] <= 0) return;   // no live row reads this request's rules
     const int row0 = pv.req_row0[b];
-    const int o = min(max(pv.row_pos[row0], 0), T_max);
+    const int o = rules.params ? min(max(pv.row_pos[row0], 0), T_max) : 0;
     const int prompt = st[b].prompt_len;
     const int32_t* tok = tokens + (size_t)b * T_max;
-    uint32_t* count = rv.count + (size_t)b * rv.words * 32;
-    float* bias = rv.bias + (size_t)b * rv.words * 32;
 
-    float4 rec = make_float4(1.f, 0.f, 0.f, 1.f);
+    fb_rule_params p{1.f, 0.f, 0.f, 0};
     bool bad = false;
     if (rules.params) {
-        const fb_rule_params p = rules.params[b];
-        rec = make_float4(p.repetition, p.presence, p.frequency, 1.f);
+        p = rules.params[b];
         bad = !(p.repetition > 0.f) || !finite(p.repetition) || !finite(p.presence) ||
               !finite(p.frequency);
     }
@@ -72,129 +124,217 @@ rules_build_kernel(fb_logit_rules rules, const fb_req_state* __restrict__ st,
         }
     }
     if (tid == 0) s_bad = 0;
-    for (int i = tid; i < rv.words; i += kBuildThreads) s_bits[i] = 0;
+    for (int i = tid; i < words; i += kBuildThreads) s_bits[i] = 0;
     __syncthreads();
     for (int i = lo + tid; i < hi; i += kBuildThreads) {
         const int id = rules.bias_id[i];
         if (id < 0 || id >= V || (i > lo && rules.bias_id[i - 1] > id) ||
             !(rules.bias_val[i] < INFINITY))
             bad = true;
+        else if (id >= v0 && id - v0 < nv)
+            atomicOr(&s_bits[(id - v0) >> 5], 1u << (id & 31));
     }
     if (bad) s_bad = 1;
+    // a bit that is set already takes no atomic: frequent tokens would queue for it
+    each_token(tok, o, v0, nv, [&](int, int v) {
+        const uint32_t m = 1u << (v & 31);
+        if (!(s_bits[v >> 5] & m)) atomicOr(&s_bits[v >> 5], m);
+    });
     __syncthreads();
-    if (s_bad) {   // uniform
-        rec.w = 0.f;
-        if (tid == 0) {
-            rv.rec[b] = rec;
+    if (s_bad) {   // uniform, and the same in every slice
+        if (tid == 0 && v0 == 0) {
+            rv.rec[b] = make_float2(NAN, 0.f);
             record_error(pv.hdr, b, FB_DERR_RULE);
         }
         return;
     }
-    // every touched entry is written before it is counted: biased ones as not
-    // seen, then the prefix's as seen
-    const int n = rules.params ? o : 0;
-    for (int i = lo + tid; i < hi; i += kBuildThreads) count[rules.bias_id[i]] = 0;
-    __threadfence();
-    __syncthreads();
-    for (int i = tid; i < n; i += kBuildThreads) {
-        const int v = tok[i];
-        if (v < 0 || v >= V) continue;
-        count[v] = kSeen;
-        bias[v] = 0.f;
-        atomicOr(&s_bits[v >> 5], 1u << (v & 31));
+
+    // ---- ranks: each thread takes `per` neighbouring words
+    const int per = (words + kBuildThreads - 1) / kBuildThreads;
+    const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
+    uint32_t mine = 0;
+    for (int i = w0; i < w1; ++i) mine += __popc(s_bits[i]);
+    uint32_t x = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t y = __shfl_up(x, off, 64);
+        if (lane >= off) x += y;
     }
-    __threadfence();
+    if (lane == 63) s_wave[wave] = x;
     __syncthreads();
-    for (int i = tid; i < n; i += kBuildThreads) {
-        const int v = tok[i];
-        if (i >= prompt && v >= 0 && v < V) atomicAdd(&count[v], 1u);
+    uint32_t before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kBuildThreads / 64; ++w) {
+        before += w < wave ? s_wave[w] : 0;
+        total += s_wave[w];
     }
-    for (int i = lo + tid; i < hi; i += kBuildThreads) {
-        const int id = rules.bias_id[i];
-        if (i > lo && rules.bias_id[i - 1] == id) continue;
-        float s = rules.bias_val[i];
-        for (int j = i + 1; j < hi && rules.bias_id[j] == id; ++j) s += rules.bias_val[j];
-        bias[id] = s;
-        atomicOr(&s_bits[id >> 5], 1u << (id & 31));
+    uint32_t at = before + x - mine;
+    for (int i = w0; i < w1; ++i) {
+        s_rank[i] = at;
+        at += __popc(s_bits[i]);
     }
+    const bool local = total <= (uint32_t)lds_counts;
+    if (local)
+        for (uint32_t i = tid; i < total; i += kBuildThreads) s_count[i] = 0;
     __syncthreads();
-    uint32_t* bits = rv.bits + (size_t)b * rv.words;
-    for (int i = tid; i < rv.words; i += kBuildThreads) bits[i] = s_bits[i];
-    if (tid == 0) rv.rec[b] = rec;
+
+    // ---- the list's ids, the bitmap and the spans
+    uint2* adj = rv.adj + (size_t)b * rv.words * 32 + v0;
+    uint32_t* bits = rv.bits + (size_t)b * rv.words + v0 / 32;
+    uint2* spans = rv.spans + (size_t)b * rv.n_spans + v0 / kSpan;
+    for (int i = tid; i < words; i += kBuildThreads) {
+        uint32_t k = s_rank[i];
+        bits[i] = s_bits[i];
+        for (uint32_t m = s_bits[i]; m; m &= m - 1, ++k)
+            adj[k] = make_uint2(0, (uint32_t)(v0 + i * 32 + __ffs(m) - 1));
+        if (i % (kSpan / 32) == 0) {
+            const int next = i + kSpan / 32;
+            spans[i / (kSpan / 32)] = make_uint2(v0 + s_rank[i], v0 + (next < words ? s_rank[next] : total));
+        }
+    }
+    workgroup_sync();
+
+    // ---- counts (adj.x holds those that do not fit the LDS)
+    auto slot = [&](int v) {
+        return s_rank[v >> 5] + __popc(s_bits[v >> 5] & ((1u << (v & 31)) - 1));
+    };
+    each_token(tok, o, v0, nv, [&](int i, int v) {
+        const uint32_t k = slot(v);
+        if (!local) {
+            if (i >= prompt) atomicAdd(&adj[k].x, 1u);
+            else atomicOr(&adj[k].x, kSeen);
+        } else if (i >= prompt) {
+            atomicAdd(&s_count[k], 1u);
+        } else if (!(s_count[k] & kSeen)) {
+            atomicOr(&s_count[k], kSeen);
+        }
+    });
+    workgroup_sync();
+    for (uint32_t i = tid; i < total; i += kBuildThreads) {
+        // counts in memory were added to past the L1
+        const uint32_t c = local ? s_count[i]
+            : __hip_atomic_load(&adj[i].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t id = adj[i].y;
+        float bias = 0.f;
+        if (hi > lo) {
+            int l = lo, h = hi;     // first entry of the id, if it is biased
+            while (l < h) {
+                const int m = (l + h) >> 1;
+                if (rules.bias_id[m] < (int)id) l = m + 1;
+                else h = m;
+            }
+            if (l < hi && rules.bias_id[l] == (int)id) {
+                bias = rules.bias_val[l];
+                for (++l; l < hi && rules.bias_id[l] == (int)id; ++l) bias += rules.bias_val[l];
+            }
+        }
+        adj[i] = make_uint2(__float_as_uint(addend(bias, c & ~kSeen, p)), id | (c ? kSeen : 0u));
+    }
+    if (tid == 0 && v0 == 0) rv.rec[b] = make_float2(p.repetition, 1.f / p.repetition);
 }
 
-// z' of a touched token.
-__device__ inline float adjust(float z, uint32_t word, float bias, const float4& rec) {
+// z' of a touched token.  z / r is the correctly rounded quotient: z times the
+// rounded reciprocal, corrected once by its exact remainder (Markstein, "Computation
+// of elementary functions on the IBM RISC System/6000 processor", 1990).
+__device__ inline float adjust(float z, const uint2& adj, const float2& rec) {
 #pragma clang fp contract(off)
-    if (word) z = z > 0.f ? z / rec.x : z * rec.x;
-    const float add = bias - ((word & ~kSeen) ? rec.y : 0.f);
-    const float times = rec.z * (float)(word & ~kSeen);
-    return z + (add - times);
+    const float q = z * rec.y;
+    const float div = fmaf(fmaf(-q, rec.x, z), rec.y, q);
+    const float pen = z > 0.f ? div : z * rec.x;
+    return (adj.y & kSeen ? pen : z) + __uint_as_float(adj.x);
 }
 
-// top_fold of logits that may be as low as the type goes (masks of -1e9 or of
-// the lowest value).  The sum is kept relative to the rounded m log2 e; where m
-// is so large that its rounding alone moves an exponent by more than 4, that
-// reference is none.  So where a group's maximum lies below -2^26 its finite
-// values count as -2^26: beside any larger logit they weigh nothing either way,
-// and a row of nothing else ties.
+// A wave's running maximum, its place and the scaled sum (see Top), for logits
+// that may be as low as the type goes (masks of -1e9 or of the lowest value).
+//
+// The maximum is the wave's, not the lane's: among 64 lanes some lane meets a new
+// maximum of its own in nearly every group, the wave in few, and a group costs 37
+// instructions instead of 70.  A lane keeps the place where it last met it.  Both
+// are held apart for the touched tokens and the others (K of fold): the ids of
+// either come in ascending order, so the first of equal maxima stays.
+//
+// The sum is kept relative to the rounded m log2 e; where m is so large that its
+// rounding alone moves an exponent by more than 4, that reference is none.  So a
+// walk begins at m = -2^26: what lies there or below weighs nothing and is no
+// maximum.  A share that ends without a maximum is walked again, its finite values
+// counted as -2^26.
 constexpr float kLowest = -67108864.f;
 
-template <int N>
-__device__ inline void fold(Top& t, float (&f)[N], int v) {
-    const float vmax = max_of(f);
-    if (vmax < kLowest && vmax > -INFINITY) {
+struct WaveTop {
+    float m[2] = {kLowest, kLowest};               // the wave's maxima
+    float mL = scaled_ref(kLowest);                // of the larger one
+    float s = 0.f;                                 // the lane's share of the sum
+    float at[2] = {-INFINITY, -INFINITY};          // the maximum as the lane last met it
+    int idx[2] = {0x7fffffff, 0x7fffffff};         // and its id
+
+    // N logits of ids v ..; lanes that take no part pass -inf
+    template <int K, int N>
+    __device__ inline void fold(const float (&f)[N], int v) {
+#pragma clang fp contract(off)
+        const float vmax = max_of(f);
+        if (__ballot(vmax > m[K])) {
+            if (vmax > m[K]) {
+                int j0 = N - 1;
 #pragma unroll
-        for (int j = 0; j < N; ++j) f[j] = f[j] > -INFINITY ? fmaxf(f[j], kLowest) : f[j];
+                for (int j = N - 1; j >= 0; --j)
+                    if (f[j] == vmax) j0 = j;
+                at[K] = vmax;
+                idx[K] = v + j0;
+            }
+            float w = vmax;
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) w = fmaxf(w, __shfl_xor(w, off, 64));
+            m[K] = w;
+            const float nmL = fmaxf(mL, scaled_ref(w));
+            s *= __builtin_amdgcn_exp2f(mL - nmL);
+            mL = nmL;
+        }
+        float e[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(f[j], kLog2e, -mL));
+#pragma unroll
+        for (int w = 1; w < N; w <<= 1)
+#pragma unroll
+            for (int j = 0; j + w < N; j += 2 * w) e[j] += e[j + w];
+        s += e[0];
     }
-    top_fold<N>(t, f, v);
-}
+
+    // The wave's Top; every lane gets it.
+    __device__ inline Top top() const {
+        const float most = fmaxf(m[0], m[1]);
+        float sum = s;
+        int first = min(at[0] == most ? idx[0] : 0x7fffffff, at[1] == most ? idx[1] : 0x7fffffff);
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            sum += __shfl_xor(sum, off, 64);
+            first = min(first, __shfl_xor(first, off, 64));
+        }
+        return Top{most, mL, sum, first};
+    }
+};
 
 // A row's rules: what the kernels below need to adjust its logits.
 struct RowRules {
-    float4 rec;
+    float2 rec;
     const uint8_t* bits;      // touched bitmap of the request, NULL if none
+    const uint2* spans;
+    const uint2* adj;
     const uint8_t* mask;      // allowed bitmap of the row, NULL if all
-    const uint32_t* count;
-    const float* bias;
     bool none;                // nothing is allowed
 
-    // N consecutive logits from index v on (v + N <= V).
-    template <int N>
-    __device__ inline void apply(float (&f)[N], int v) const {
-        constexpr uint32_t all = (1u << N) - 1;
-        if (bits) {
-            const uint32_t t = window(bits, v, N) & all;
-            if (t) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (t >> j & 1) f[j] = adjust(f[j], count[v + j], bias[v + j], rec);
-            }
-        }
-        if (mask) {
-            const uint32_t a = window(mask, v, N) & all;
-#pragma unroll
-            for (int j = 0; j < N; ++j) f[j] = a >> j & 1 ? f[j] : -INFINITY;
-        }
-    }
-
-    // The bits from index v on, at least n <= 8 of them.
-    static __device__ inline uint32_t window(const uint8_t* p, int v, int n) {
-        const uint32_t w = p[v >> 3] | (uint32_t)p[(v + n - 1) >> 3] << 8;
-        return w >> (v & 7);
-    }
+    // the bits of the eight tokens from v on (v a multiple of 8)
+    __device__ inline uint32_t allowed(int v) const { return mask ? mask[v >> 3] : 255u; }
 };
 
 __device__ inline RowRules row_rules(const fb_logit_rules& rules, const RuleView& rv,
                                      const PackView& pv, int row, int req, int mask_words) {
     RowRules r;
     r.rec = rv.rec[req];
-    const size_t at = (size_t)req * rv.words;
     r.bits = rules.params || rules.bias_start
-                 ? reinterpret_cast<const uint8_t*>(rv.bits + at) : nullptr;
-    r.count = rv.count + at * 32;
-    r.bias = rv.bias + at * 32;
-    r.none = r.rec.w == 0.f;
+                 ? reinterpret_cast<const uint8_t*>(rv.bits + (size_t)req * rv.words) : nullptr;
+    r.spans = rv.spans + (size_t)req * rv.n_spans;
+    r.adj = rv.adj + (size_t)req * rv.words * 32;
+    r.none = isnan(r.rec.x);
     r.mask = nullptr;
     if (rules.masks) {
         const int m = rules.row_mask[row];
@@ -209,77 +349,307 @@ __device__ inline RowRules row_rules(const fb_logit_rules& rules, const RuleView
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kVocabThreads)
+__device__ inline float value(T x) {
+    if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)x << 16);
+    else return x;
+}
+template <typename T>
+__device__ inline T minus_inf() {
+    if constexpr (sizeof(T) == 2) return (T)0xff80;
+    else return -INFINITY;
+}
+
+// Rows of a vocabulary that is no multiple of eight start anywhere; the address
+// unit takes misaligned 16 bytes.
+typedef unsigned Words16 __attribute__((ext_vector_type(4), aligned(2)));
+
+// Eight logits.
+template <typename T>
+struct Eight {
+    static constexpr int Q = sizeof(T) / 2;
+    uint4 q[Q];
+
+    __device__ inline void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const Words16 x = __builtin_nontemporal_load(reinterpret_cast<const Words16*>(p) + i);
+            q[i] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+    }
+    __device__ inline void load(const T* p, int n) {     // n elements, the others -inf
+        T t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = i < n ? p[i] : minus_inf<T>();
+        __builtin_memcpy(q, t, sizeof t);
+    }
+    __device__ inline void store(T* p, int n) const {
+        if (n >= 8) {
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+                __builtin_nontemporal_store(Words16{q[i].x, q[i].y, q[i].z, q[i].w},
+                                            reinterpret_cast<Words16*>(p) + i);
+        } else {
+            T t[8];
+            __builtin_memcpy(t, q, sizeof t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) p[i] = t[i];
+        }
+    }
+    __device__ inline void unpack(float (&f)[8]) const {
+        if constexpr (sizeof(T) == 2) {
+            VecTraits<uint16_t>::unpack(q[0], f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f[4 * i] = __uint_as_float(q[i].x);
+                f[4 * i + 1] = __uint_as_float(q[i].y);
+                f[4 * i + 2] = __uint_as_float(q[i].z);
+                f[4 * i + 3] = __uint_as_float(q[i].w);
+            }
+        }
+    }
+    static __device__ inline uint32_t pick(uint32_t m, uint32_t a, uint32_t b) {
+        return (m & a) | (~m & b);
+    }
+    // -inf where a bit of `keep` is 0
+    __device__ inline void mask(uint32_t keep) {
+        auto bit = [&](int i) { return (uint32_t)__builtin_amdgcn_sbfe(keep, i, 1); };
+        if constexpr (sizeof(T) == 2) {
+            auto word = [&](int i, uint32_t x) {   // two bits' signs, a half word each
+                return pick(__builtin_amdgcn_perm(bit(2 * i + 1), bit(2 * i), 0x05040100u), x,
+                            0xff80ff80u);
+            };
+            q[0] = make_uint4(word(0, q[0].x), word(1, q[0].y), word(2, q[0].z), word(3, q[0].w));
+        } else {
+            const uint32_t inf = 0xff800000u;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                q[i] = make_uint4(pick(bit(4 * i), q[i].x, inf), pick(bit(4 * i + 1), q[i].y, inf),
+                                  pick(bit(4 * i + 2), q[i].z, inf),
+                                  pick(bit(4 * i + 3), q[i].w, inf));
+        }
+    }
+};
+
+// A row's workgroups take its pieces of 32 KB in turn; of a piece a wave takes a
+// window of 4 KB, a lane kBatch groups of eight logits.
+template <typename T>
+struct Window {
+    static constexpr int kBatch = kVocabBatch * 2 / sizeof(T);
+    static constexpr int kTokens = kBatch * 512;
+    static constexpr int kPiece = kTokens * (kVocabThreads / 64);
+    static_assert(kTokens % kSpan == 0 && kSlice % kTokens == 0);
+    typedef T Stage[kTokens];
+
+    Eight<T> raw[kBatch];
+
+    // What lies past the row comes out as -inf.
+    __device__ inline void load(const T* rp, int v0, int V) {
+        const int base = v0 + (threadIdx.x & 63) * 8;
+        if (v0 + kTokens <= V) {   // uniform
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) raw[j].load(rp + base + j * 512);
+            return;
+        }
+        fill();
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int v = base + j * 512;
+            if (v + 8 <= V) raw[j].load(rp + v);
+            else if (v < V) raw[j].load(rp + v, V - v);
+        }
+    }
+    __device__ inline void fill() {
+        const uint32_t inf = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+#pragma unroll
+            for (int i = 0; i < Eight<T>::Q; ++i) raw[j].q[i] = make_uint4(inf, inf, inf, inf);
+    }
+    // the lane's bytes of the row's mask, none past the row
+    struct Allowed {
+        uint32_t b[kBatch];
+
+        __device__ inline void load(const uint8_t* mask, int v0, int V) {
+            if (v0 + kTokens <= V) {   // uniform
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+                    b[j] = (mask + (v0 >> 3))[(threadIdx.x & 63) + j * 64];
+                return;
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int v = v0 + j * 512 + (threadIdx.x & 63) * 8;
+                b[j] = v < V ? mask[v >> 3] : 0;
+                if (v + 8 > V && v < V) b[j] &= (1u << (V - v)) - 1;
+            }
+        }
+        __device__ inline bool some() const {   // uniform
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) m |= b[j];
+            return __ballot(m != 0) != 0;
+        }
+    };
+    // -inf where the mask forbids it
+    __device__ inline void mask(const Allowed& allowed) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (__ballot(allowed.b[j] != 255)) raw[j].mask(allowed.b[j]);
+    }
+    __device__ inline void stage(Stage& s) const {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            __builtin_memcpy(&s[j * 512 + (threadIdx.x & 63) * 8], raw[j].q, sizeof raw[j].q);
+    }
+    __device__ inline void fetch(const Stage& s) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            __builtin_memcpy(raw[j].q, &s[j * 512 + (threadIdx.x & 63) * 8], sizeof raw[j].q);
+    }
+};
+
+// The entries of the wave's windows: lane i has the first of its i-th window's,
+// lane 32 + i one past the last (at most 32 windows: V is at most 2^19).
+template <typename T>
+__device__ inline uint32_t window_entries(const RowRules& rr, int first, int stride, int V) {
+    if (!rr.bits) return 0;
+    const int lane = threadIdx.x & 63;
+    const int v0 = first + (lane & 31) * stride;
+    if (v0 >= V) return 0;
+    const int last = min((v0 + Window<T>::kTokens) / kSpan, (V + kSpan - 1) / kSpan) - 1;
+    return lane < 32 ? rr.spans[v0 / kSpan].x : rr.spans[last].y;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kVocabThreads, 8)
 vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
                    fb_logit_rules rules, RuleView rv, int mask_words,
                    float4* __restrict__ part) {
-    using VT = VecTraits<T>;
-    constexpr int N = VT::N;
-    constexpr int kBatch = kVocabBatch;
+    using W = Window<T>;
+    __shared__ __attribute__((aligned(16))) typename W::Stage stages[kVocabThreads / 64];
+    __shared__ Top wtop[kVocabThreads / 64];
+    __shared__ int s_met[kVocabThreads / 64];
     const int row = blockIdx.x / nsplit;
     const int k = blockIdx.x % nsplit;
     const int req = pv.row_req[row];
     if (req < 0) return;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const RowRules rr = row_rules(rules, rv, pv, row, req, mask_words);
     if (rr.none) {
         if (tid == 0) part[(size_t)row * nsplit + k] = top_pack(top_empty());
         return;
     }
     const T* rp = logits + (size_t)row * V;
-    const size_t abs0 = (size_t)row * V;
-    int a = (int)((N - (abs0 % N)) % N);
-    if (a > V) a = V;
-    const int e = a + ((V - a) / N) * N;
+    const int first = k * W::kPiece + wave * W::kTokens;
+    const int stride = nsplit * W::kPiece;
+    const uint32_t entries = window_entries<T>(rr, first, stride, V);
+    typename W::Stage& stage = stages[wave];
 
-    Top t = top_empty();
-    if (k == 0 && tid < a) {
-        float f[1] = {VT::scalar(rp + tid)};
-        rr.template apply<1>(f, tid);
-        fold<1>(t, f, tid);
-    }
-    const int stride = kVocabThreads * N;
-    const int piece = kBatch * stride;
-    for (int base = a + k * piece + tid * N; base < e; base += nsplit * piece) {
-        uint4 raw[kBatch];
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-            const int v = base + j * stride;
-            raw[j] = v < e ? load_stream16(rp + v) : make_uint4(0, 0, 0, 0);
+    WaveTop wt;
+    // The mask's bytes come a window ahead: of a window that allows nothing the
+    // logits are not read.
+    typename W::Allowed allowed, next;
+    if (rr.mask) next.load(rr.mask, first, V);
+    bool any = false;     // something is allowed
+    int i = 0;
+    for (int v0 = first; v0 < V; v0 += stride, ++i) {
+        if (rr.mask) {    // uniform
+            allowed = next;
+            const bool some = allowed.some();
+            if (v0 + stride < V) next.load(rr.mask, v0 + stride, V);
+            if (!some) continue;
+        }
+        any = true;
+        const int e0 = __builtin_amdgcn_readlane(entries, i);
+        const int e1 = __builtin_amdgcn_readlane(entries, 32 + i);
+        W w;
+        w.load(rp, v0, V);
+        uint2 adj = make_uint2(0, (uint32_t)v0);
+        if (e0 + lane < e1) adj = rr.adj[e0 + lane];
+        if (rr.mask) w.mask(allowed);
+        if (e1 > e0) {   // uniform
+            // the touched tokens are taken out of the staged window, adjusted and
+            // folded one a lane; the rest folds below
+            w.stage(stage);
+            for (int e = e0; e < e1; e += 64) {
+                const uint2 a = adj;
+                if (e + 64 + lane < e1) adj = rr.adj[e + 64 + lane];
+                const int v = (int)(a.y & ~kSeen);
+                float f[1] = {-INFINITY};
+                if (e + lane < e1) {
+                    T& z = stage[v - v0];
+                    f[0] = adjust(value(z), a, rr.rec);
+                    z = minus_inf<T>();
+                }
+                wt.fold<1, 1>(f, v);
+            }
+            w.fetch(stage);
         }
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-            const int v = base + j * stride;
-            if (v < e) {
-                float f[N];
-                VT::unpack(raw[j], f);
-                rr.template apply<N>(f, v);
-                fold<N>(t, f, v);
+        for (int j = 0; j < W::kBatch; ++j) {
+            float f[8];
+            w.raw[j].unpack(f);
+            wt.fold<0, 8>(f, v0 + j * 512 + lane * 8);
+        }
+    }
+
+    Top t = wt.top();
+    // the workgroup's partial: its waves' in order, by the first wave
+    auto write = [&]() {
+        if (lane == 0) wtop[wave] = t;
+        __syncthreads();
+        if (wave != 0) return;
+        t = lane < kVocabThreads / 64 ? wtop[lane] : top_empty();
+#pragma unroll
+        for (int off = 1; off < kVocabThreads / 64; off <<= 1) {
+            Top o;
+            o.m = __shfl_xor(t.m, off, 64);
+            o.mL = __shfl_xor(t.mL, off, 64);
+            o.s = __shfl_xor(t.s, off, 64);
+            o.idx = __shfl_xor(t.idx, off, 64);
+            t = top_merge(t, o);
+        }
+        if (lane == 0) part[(size_t)row * nsplit + k] = top_pack(t);
+    };
+    // whether some wave met a maximum, and whether anything is allowed
+    if (lane == 0) s_met[wave] = (t.m > kLowest ? 1 : 0) | (any ? 2 : 0);
+    write();
+    int met = 0;
+#pragma unroll
+    for (int w = 0; w < kVocabThreads / 64; ++w) met |= s_met[w];
+    if (met & 1) return;   // uniform
+    t = top_empty();
+    if (met & 2) {
+        const float each = __builtin_amdgcn_exp2f(fmaf(kLowest, kLog2e, -scaled_ref(kLowest)));
+        auto take = [&](int v, float z) {
+            if (z > -INFINITY) t = Top{kLowest, scaled_ref(kLowest), t.s + each, min(t.idx, v)};
+        };
+        i = 0;
+        for (int v0 = first; v0 < V; v0 += stride, ++i) {
+            const int end = min(v0 + W::kTokens, V);
+            for (int v = v0 + lane; v < end; v += 64)
+                if ((rr.allowed(v & ~7) >> (v & 7) & 1) &&
+                    !(rr.bits && rr.bits[v >> 3] >> (v & 7) & 1))
+                    take(v, value(rp[v]));
+            const int e1 = __builtin_amdgcn_readlane(entries, 32 + i);
+            for (int e = __builtin_amdgcn_readlane(entries, i) + lane; e < e1; e += 64) {
+                const uint2 a = rr.adj[e];
+                const int v = (int)(a.y & ~kSeen);
+                if (rr.allowed(v & ~7) >> (v & 7) & 1) take(v, adjust(value(rp[v]), a, rr.rec));
             }
         }
-    }
-    if (k == 0 && tid < V - e) {
-        float f[1] = {VT::scalar(rp + e + tid)};
-        rr.template apply<1>(f, e + tid);
-        fold<1>(t, f, e + tid);
-    }
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        Top o;
-        o.m = __shfl_xor(t.m, off, 64);
-        o.mL = __shfl_xor(t.mL, off, 64);
-        o.s = __shfl_xor(t.s, off, 64);
-        o.idx = __shfl_xor(t.idx, off, 64);
-        t = top_merge(t, o);
+        for (int off = 32; off > 0; off >>= 1) {
+            t.s += __shfl_xor(t.s, off, 64);
+            t.idx = min(t.idx, __shfl_xor(t.idx, off, 64));
+        }
+        if (t.s > 0.f) t = Top{kLowest, scaled_ref(kLowest), t.s, t.idx};
     }
-    __shared__ Top wtop[kVocabThreads / 64];
-    if ((tid & 63) == 0) wtop[tid >> 6] = t;
     __syncthreads();
-    if (tid == 0) {
-        Top r = wtop[0];
-        for (int w = 1; w < kVocabThreads / 64; ++w) r = top_merge(r, wtop[w]);
-        part[(size_t)row * nsplit + k] = top_pack(r);
-    }
+    write();
 }
 
 // (p, x_hat) of every live row from its partials, as the update merges them.
@@ -303,46 +673,103 @@ template <typename T>
 __global__ void __launch_bounds__(kVocabThreads)
 logits_rules_kernel(const T* logits, T* out, int V, int nsplit, PackView pv,
                     fb_logit_rules rules, RuleView rv, int mask_words) {
-    using VT = VecTraits<T>;
+    using W = Window<T>;
+    __shared__ __attribute__((aligned(16))) typename W::Stage stages[kVocabThreads / 64];
     const int row = blockIdx.x / nsplit;
     const int k = blockIdx.x % nsplit;
     const int req = pv.row_req[row];
     if (req < 0) return;
-    const RowRules rr = row_rules(rules, rv, pv, row, req, mask_words);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    RowRules rr = row_rules(rules, rv, pv, row, req, mask_words);
+    if (rr.none) rr.bits = nullptr;
     const T* rp = logits + (size_t)row * V;
     T* wp = out + (size_t)row * V;
-    for (int v = k * kVocabThreads + threadIdx.x; v < V; v += nsplit * kVocabThreads) {
-        float f[1] = {VT::scalar(rp + v)};
-        rr.template apply<1>(f, v);
-        if (rr.none) f[0] = -INFINITY;
-        if constexpr (sizeof(T) == 2) {
-            const __bf16 r = (__bf16)f[0];
-            wp[v] = __builtin_bit_cast(uint16_t, r);
-        } else {
-            wp[v] = f[0];
+    const int first = k * W::kPiece + wave * W::kTokens;
+    const int stride = nsplit * W::kPiece;
+    const uint32_t entries = window_entries<T>(rr, first, stride, V);
+    typename W::Stage& stage = stages[wave];
+
+    typename W::Allowed allowed, next;
+    if (rr.mask) next.load(rr.mask, first, V);
+    int i = 0;
+    for (int v0 = first; v0 < V; v0 += stride, ++i) {
+        bool some = !rr.none;
+        if (rr.mask) {    // uniform, and a window ahead as above
+            allowed = next;
+            some &= allowed.some();
+            if (v0 + stride < V) next.load(rr.mask, v0 + stride, V);
+        }
+        const int e0 = __builtin_amdgcn_readlane(entries, i);
+        const int e1 = some ? __builtin_amdgcn_readlane(entries, 32 + i) : e0;
+        W w;
+        if (some) w.load(rp, v0, V);
+        else w.fill();
+        uint2 adj = make_uint2(0, (uint32_t)v0);
+        if (e0 + lane < e1) adj = rr.adj[e0 + lane];
+        if (some && rr.mask) w.mask(allowed);
+        if (e1 > e0) {   // uniform
+            w.stage(stage);
+            for (int e = e0; e < e1; e += 64) {
+                const uint2 a = adj;
+                if (e + 64 + lane < e1) adj = rr.adj[e + 64 + lane];
+                if (e + lane < e1) {
+                    T& z = stage[(int)(a.y & ~kSeen) - v0];
+                    const float f = adjust(value(z), a, rr.rec);
+                    if constexpr (sizeof(T) == 2) z = __builtin_bit_cast(uint16_t, (__bf16)f);
+                    else z = f;
+                }
+            }
+            w.fetch(stage);
+        }
+#pragma unroll
+        for (int j = 0; j < W::kBatch; ++j) {
+            const int v = v0 + j * 512 + lane * 8;
+            if (v < V) w.raw[j].store(wp + v, V - v);
         }
     }
 }
+
+// Slices of the vocabulary per request: workgroups for about every CU, each of
+// at least 8192 tokens (a workgroup reads the whole prefix).
+int build_slices(int B, int V, int cu_count) {
+    int n = cu_count / B;
+    if (n > V / 8192) n = V / 8192;
+    return n < 1 ? 1 : n > 32 ? 32 : n;
+}
+
+constexpr int kBuildLds = 156 * 1024;
 
 }  // namespace
 
 RulesSizes rules_sizes(const fb_pack* pack, int V) {
     RulesSizes z{};
     z.words = (V + 127) / 128 * 4;
+    z.spans = (V + kSpan - 1) / kSpan;
     const size_t B = pack->B;
-    z.off_bits = (B * sizeof(float4) + 255) / 256 * 256;
-    z.off_count = z.off_bits + (B * z.words * 4 + 255) / 256 * 256;
-    z.off_bias = z.off_count + B * z.words * 32 * 4;
-    z.total = z.off_bias + B * z.words * 32 * 4;
+    z.off_bits = (B * sizeof(float2) + 255) / 256 * 256;
+    z.off_spans = z.off_bits + (B * z.words * 4 + 255) / 256 * 256;
+    z.off_adj = z.off_spans + (B * z.spans * sizeof(uint2) + 255) / 256 * 256;
+    z.total = z.off_adj + B * z.words * 32 * sizeof(uint2);
     return z;
 }
 
 hipError_t launch_rules_build(const fb_logit_rules* rules, const fb_req_state* st,
                               const int32_t* tokens, int T_max, int V, const fb_pack* pack,
-                              void* ws, const RulesSizes& z, hipStream_t stream) {
-    hipLaunchKernelGGL(rules_build_kernel, dim3(pack->B), dim3(kBuildThreads),
-                       (size_t)z.words * 4, stream, *rules, st, tokens, T_max, V,
-                       pack_view(pack), rule_view(z, ws));
+                              void* ws, const RulesSizes& z, int cu_count, hipStream_t stream) {
+    const int n = build_slices(pack->B, V, cu_count);
+    const int slice = ((V + n - 1) / n + kSlice - 1) / kSlice * kSlice;
+    const int slices = (V + slice - 1) / slice;
+    const int words = ((V < slice ? V : slice) + 31) / 32;
+    // counts for as many tokens as a prefix and its biases can touch, at most
+    // what is left of the LDS
+    long long counts = (kBuildLds - words * 8) / 4;
+    const long long most = (long long)T_max + rules->n_bias;
+    if (counts > most) counts = most;
+    if (counts > words * 32) counts = words * 32;
+    hipLaunchKernelGGL(rules_build_kernel, dim3(pack->B * slices), dim3(kBuildThreads),
+                       (size_t)words * 8 + (size_t)counts * 4, stream, *rules, st, tokens, T_max, V,
+                       pack_view(pack), rule_view(z, ws), slice, slices, (int)counts);
     return hipGetLastError();
 }
 

@@ -155,17 +155,19 @@ def test_empty_rows_and_spoiled_masked_places():
     """Masks that leave nothing or one token; masked entries hold NaN and
     infinities; allowed ones -inf and the type's lowest value."""
     V = 4099
-    for dtype in ("bf16", "f32"):
+    for dtype, lowest in (("bf16", None), ("f32", None), ("f32", -1e9), ("bf16", -2.0 ** 26)):
         bt = Batch(**BATCHES["ragged"], V=V).cuda()
         rules = Rules(bt, V, seed=2, n_masks=4, keep=(0.0, 0.3, 0.3, 0.0))
         rules.allowed[3, 4098] = True
         rules.masks = np.packbits(np.pad(rules.allowed, ((0, 0), (0, -V % 32))), axis=1,
                                   bitorder="little").view(np.int32)
         z = logits(bt, V, dtype)
-        low = torch.finfo(TORCH[dtype]).min
+        low = torch.finfo(TORCH[dtype]).min if lowest is None else lowest
         z[:, ::5] = -float("inf")
         z[:, 1::5] = low
-        z[bt.live[-1], :] = low if rules.row_mask[bt.live[-1]] < 0 else z[bt.live[-1], :]
+        z[bt.live[-4:], 10:] = low              # nothing but such values past the tenth
+        z[bt.live[-4:], :10] = -float("inf")
+        rules.row_mask[bt.live[-4:]] = [-1, 1, 2, -1]
         for row in bt.live:
             m = rules.row_mask[row]
             if m >= 0:
@@ -189,6 +191,24 @@ def test_ties_take_the_lowest_id():
         rules.masks = np.packbits(rules.allowed, axis=1, bitorder="little").view(np.int32)
         run = Run(bt, V, "bf16", rules, z).go()
         assert run.argmax[bt.live[0]].item() == min(at)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ties_of_touched_and_untouched_tokens(dtype):
+    """Equal z' of tokens that go through the rules and tokens that do not, in
+    every order: the lowest id wins."""
+    V, rng = 60000, np.random.default_rng(5)
+    for trial in range(12):
+        at = np.sort(rng.choice(V, 6, replace=False)) if trial % 2 else \
+            rng.integers(0, V - 64) + np.sort(rng.choice(64, 6, replace=False))
+        tokens = np.concatenate([rng.permutation(at)[:3], rng.integers(0, V, 37)])[None]
+        bt = Batch(w=[1], o=[40], bl=1, W_max=1, tokens=np.pad(tokens, ((0, 0), (0, 20))), V=V).cuda()
+        rules = Rules(bt, V, seed=trial, n_bias=None, n_masks=0)
+        rules.params[:] = [1, 0, 0, 0]          # touched and left as they are
+        z = torch.randn(bt.row_cap, V, device="cuda").to(TORCH[dtype])
+        z[:, at] = 9.0
+        run = Run(bt, V, dtype, rules, z).go()
+        assert run.argmax.item() == at[0]
 
 
 def test_in_place():
@@ -243,11 +263,25 @@ def test_bad_rules_are_recorded_and_allow_nothing(spoil):
 
 
 def test_largest_vocabulary():
-    """V = 2^20, the most the call takes."""
-    V = 1 << 20
+    """V = 2^19, the most the call takes."""
+    V = 1 << 19
     bt = Batch(**BATCHES["token"], V=V).cuda()
     rules = Rules(bt, V, seed=1, n_masks=2, keep=(0.5, 0.9))
     rules.row_mask[:] = 1
+    z = logits(bt, V, "bf16")
+    check(bt, V, "bf16", rules, z, Run(bt, V, "bf16", rules, z).go())
+
+
+def test_more_touched_tokens_than_fit_the_lds():
+    """Many requests (one build workgroup each) over the largest vocabulary, one
+    of them with a prefix of many different tokens."""
+    V, B, rng = 1 << 19, 130, np.random.default_rng(7)
+    o = np.full(B, 20)
+    o[5] = 16000
+    tokens = rng.integers(0, V, size=(B, 16004))
+    bt = Batch(w=[1] * B, o=o, bl=1, W_max=1, tokens=tokens, V=V, prompt=[9000 if b == 5 else 7 for b in range(B)],
+               inactive=[b for b in range(B) if b not in (0, 5, 129)]).cuda()
+    rules = Rules(bt, V, seed=1, n_bias=40, n_masks=1, keep=(0.9,))
     z = logits(bt, V, "bf16")
     check(bt, V, "bf16", rules, z, Run(bt, V, "bf16", rules, z).go())
 

@@ -127,7 +127,7 @@ def test_rules_calls_refuse(lib, pack):
     need = lib.fb_rules_workspace_bytes(ph, 1000)
     assert need > 0 and need % 16 == 0
     assert lib.fb_rules_workspace_bytes(ph, 0) == 0
-    assert lib.fb_rules_workspace_bytes(ph, (1 << 20) + 1) == 0
+    assert lib.fb_rules_workspace_bytes(ph, (1 << 19) + 1) == 0
     assert lib.fb_rules_workspace_bytes(None, 1000) == 0
     upd = lib.fb_update_workspace_bytes(ph, 1000)
 
@@ -135,7 +135,7 @@ def test_rules_calls_refuse(lib, pack):
         return lib.fb_rules_build(rules, st, tok, T, V, p, ws, nb, None)
     assert build(rules=None) == build(st=None) == build(tok=None) == build(T=0) == fb.FB_E_INVAL
     assert build(V=0) == build(p=None) == build(ws=OFF8) == fb.FB_E_INVAL
-    assert build(V=(1 << 20) + 1) == fb.FB_E_UNSUPPORTED
+    assert build(V=(1 << 19) + 1) == fb.FB_E_UNSUPPORTED
     assert build(ws=None) == build(nb=need - 1) == fb.FB_E_WORKSPACE
 
     def reduce(z=P, V=1000, dt=1, p=ph, rules=r, ws=P, nb=need, uw=P, ub=upd, c=P, am=P):
