@@ -26,6 +26,7 @@ constexpr int kBuildThreads = 1024;
 constexpr int kSpan = 1024;               // tokens whose list entries are found by one lookup
 constexpr int kSlice = 2 * kSpan;         // slices of the build are multiples of it
 constexpr uint32_t kSeen = 0x80000000u;   // beside a count or an id: the token is seen
+constexpr uint32_t kDone = 0x40000000u;   // beside an id, within the build: a bias is in
 
 // What fb_rules_build leaves of request b:
 //   rec    repetition (NaN if the rules are unsound) and its reciprocal
@@ -67,20 +68,43 @@ __device__ inline void workgroup_sync() {
 }
 
 // Calls f(i, token - v0) for the tokens of [0, n) that lie in [v0, v0 + nv), the
-// loads of eight rounds in flight together.
+// loads of eight rounds in flight together: one token a load up to 8192 of them
+// (one round trip, every lane at work), four neighbours beyond.
 template <typename F>
 __device__ inline void each_token(const int32_t* tok, int n, int v0, int nv, F&& f) {
-    constexpr int U = 8;
-    for (int i0 = threadIdx.x; i0 < n; i0 += U * kBuildThreads) {
+    typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));
+    constexpr int U = 8, kRound = 4 * kBuildThreads;
+    if (n <= U * kBuildThreads) {
         int v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * kBuildThreads;
+            const int i = threadIdx.x + u * kBuildThreads;
             v[u] = i < n ? tok[i] : -1;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (v[u] >= v0 && v[u] - v0 < nv) f(i0 + u * kBuildThreads, v[u] - v0);
+            if (v[u] >= v0 && v[u] - v0 < nv) f((int)threadIdx.x + u * kBuildThreads, v[u] - v0);
+        return;
+    }
+    for (int i0 = threadIdx.x * 4; i0 < n; i0 += U * kRound) {
+        i32x4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * kRound;
+            v[u] = i32x4{-1, -1, -1, -1};
+            if (i + 4 <= n) {
+                v[u] = *reinterpret_cast<const i32x4*>(tok + i);
+            } else if (i < n) {
+                v[u][0] = tok[i];
+                if (i + 1 < n) v[u][1] = tok[i + 1];
+                if (i + 2 < n) v[u][2] = tok[i + 2];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (v[u][j] >= v0 && v[u][j] - v0 < nv) f(i0 + u * kRound + j, v[u][j] - v0);
     }
 }
 
@@ -210,25 +234,32 @@ rules_build_kernel(fb_logit_rules rules, const fb_req_state* __restrict__ st,
         }
     });
     workgroup_sync();
+    // ---- entries without a bias, then those that have one
     for (uint32_t i = tid; i < total; i += kBuildThreads) {
         // counts in memory were added to past the L1
         const uint32_t c = local ? s_count[i]
             : __hip_atomic_load(&adj[i].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         const uint32_t id = adj[i].y;
-        float bias = 0.f;
-        if (hi > lo) {
-            int l = lo, h = hi;     // first entry of the id, if it is biased
-            while (l < h) {
-                const int m = (l + h) >> 1;
-                if (rules.bias_id[m] < (int)id) l = m + 1;
-                else h = m;
-            }
-            if (l < hi && rules.bias_id[l] == (int)id) {
-                bias = rules.bias_val[l];
-                for (++l; l < hi && rules.bias_id[l] == (int)id; ++l) bias += rules.bias_val[l];
-            }
+        adj[i] = make_uint2(local ? __float_as_uint(addend(0.f, c & ~kSeen, p)) : c,
+                            id | (c ? kSeen : 0u));
+    }
+    workgroup_sync();
+    for (int i = lo + tid; i < hi; i += kBuildThreads) {
+        const int id = rules.bias_id[i];
+        if (id < v0 || id - v0 >= nv || (i > lo && rules.bias_id[i - 1] == id)) continue;
+        float bias = rules.bias_val[i];
+        for (int j = i + 1; j < hi && rules.bias_id[j] == id; ++j) bias += rules.bias_val[j];
+        const uint32_t k = slot(id - v0);
+        if (local) adj[k].x = __float_as_uint(addend(bias, s_count[k] & ~kSeen, p));
+        else adj[k] = make_uint2(__float_as_uint(addend(bias, adj[k].x & ~kSeen, p)), adj[k].y | kDone);
+    }
+    if (!local) {
+        workgroup_sync();
+        for (uint32_t i = tid; i < total; i += kBuildThreads) {
+            const uint2 e = adj[i];
+            adj[i] = e.y & kDone ? make_uint2(e.x, e.y & ~kDone)
+                                 : make_uint2(__float_as_uint(addend(0.f, e.x & ~kSeen, p)), e.y);
         }
-        adj[i] = make_uint2(__float_as_uint(addend(bias, c & ~kSeen, p)), id | (c ? kSeen : 0u));
     }
     if (tid == 0 && v0 == 0) rv.rec[b] = make_float2(p.repetition, 1.f / p.repetition);
 }
