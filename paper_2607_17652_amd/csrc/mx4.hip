@@ -24,6 +24,7 @@ namespace {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 8;
@@ -102,29 +103,51 @@ __device__ inline void dma16(uint32_t lds, const void* p) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
                  :: "s"(lds), "v"(p) : "memory");
 }
+__device__ inline void dma4(uint32_t lds, uint32_t off, const void* base) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2"
+                 :: "s"(lds), "v"(off), "s"(base) : "memory");
+}
 __device__ inline void dma1(uint32_t lds, uint32_t off, const void* base) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_ubyte %1, %2"
                  :: "s"(lds), "v"(off), "s"(base) : "memory");
 }
 
+// A NaN scale makes its column NaN: lanes r, r + 16, .. hold the flags of the
+// tile's column r, lane group g the columns 4 g ...
+template <int TT, int NT>
+__device__ inline void spoil(f32x4 (&acc)[TT][NT], int n, bool nan, int g) {
+    uint64_t m = __ballot(nan);
+    if (!m) return;
+    m |= m >> 32;
+    m |= m >> 16;
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (m >> (4 * g + i) & 1) acc[t][n][i] = __uint_as_float(0x7fc00000u);
+}
+
 // TT 16-token tiles, NT 16-column tiles a wave, KW waves to a tile.
-template <int TT, int NT, int KW>
+// DW: whole chunks (K a multiple of 128) and scales 4-byte aligned, so that a row's
+// four scales of a chunk are one dword; a byte a lane otherwise.
+template <int TT, int NT, int KW, bool DW>
 struct MxShape {
     static constexpr int kX = KW * TT * 4096;               // x of a stage
-    static constexpr int kW = NT * 1280;                    // a wave's codes and scales
+    static constexpr int kScaleOps = DW ? (NT + 3) / 4 : NT;
+    static constexpr int kW = NT * 1024 + kScaleOps * 256;  // a wave's codes and scales
     static constexpr int kStage = kX + kWaves * kW;
     static constexpr int kFit = kLdsBytes / kStage;
     static constexpr int kStages = kFit > 4 ? 4 : kFit;
     static constexpr int kXOps = KW * TT > 2 ? KW * TT / 2 : 1;   // x loads per wave and stage
-    static constexpr int kOps = kXOps + 2 * NT;
+    static constexpr int kOps = kXOps + NT + kScaleOps;
     static_assert(kStages >= 2 && (kStages - 2) * kOps < 64 && (KW == 1 || NT == 1));
     static_assert(KW == 1 || kWaves * TT * 1024 <= kStages * kStage);
 };
 
-template <int TT, int NT, int KW>
+template <int TT, int NT, int KW, bool DW>
 __global__ void __launch_bounds__(kMxThreads)
 mx4_kernel(MxArgs a, PackView pv, int n_groups) {
-    using S = MxShape<TT, NT, KW>;
+    using S = MxShape<TT, NT, KW, DW>;
     __shared__ __attribute__((aligned(16))) unsigned char lds[S::kStages * S::kStage];
     const int ng = blockIdx.x % n_groups;
     const int r0 = blockIdx.x / n_groups * (TT * 16);
@@ -149,9 +172,15 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
     const int nb = min(n0, a.N - 1);
     const uint8_t* cbase = a.codes + (size_t)nb * (a.K / 2);
     const uint8_t* sbase = a.scales + (size_t)nb * (a.K / 32);
-    int nrow[NT];
+    const int last = a.N - 1 - nb;
+    uint32_t c_off[NT], s_off[S::kScaleOps];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) nrow[n] = min(n * 16 + wr, a.N - 1 - nb);
+    for (int n = 0; n < NT; ++n)
+        c_off[n] = (uint32_t)min(n * 16 + wr, last) * (uint32_t)(a.K / 2);
+#pragma unroll
+    for (int o = 0; o < S::kScaleOps; ++o)
+        s_off[o] = (uint32_t)min(DW ? min(o * 64 + lane, NT * 16 - 1) : o * 16 + wr, last) *
+                   (uint32_t)(a.K / 32);
     const uint16_t* xbase = a.x + (size_t)r0 * a.K;
     uint32_t x_off[S::kXOps];
     int x_cc[S::kXOps];
@@ -169,7 +198,7 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
         for (int i = 0; i < S::kXOps; ++i) {
             const int o = (wave * S::kXOps + i) % (KW * TT * 4);
             const int c = min(s * KW + x_cc[i], C - 1);
-            if (c * 128 + 128 <= a.K) {
+            if (DW || c * 128 + 128 <= a.K) {
                 dma16(at + o * 1024, x_off[i], xbase + c * 128);
             } else {
                 const int r = (o % (TT * 4)) * 4 + (lane >> 4);
@@ -182,15 +211,16 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
         }
         const int c = min(s * KW + kq, C - 1);
         // a group past K reads the chunk's first one in its place
-        const int piece = (4 * c + wp) * 32 < a.K ? wp : 0;
-        const int byte = (4 * c + (lane & 3)) * 32 < a.K ? (lane & 3) : 0;
+        const int piece = DW || (4 * c + wp) * 32 < a.K ? wp : 0;
+        const int byte = DW || (4 * c + (lane & 3)) * 32 < a.K ? (lane & 3) : 0;
         const uint32_t mine = at + S::kX + wave * S::kW;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            dma16(mine + n * 1024, (uint32_t)nrow[n] * (uint32_t)(a.K / 2) + piece * 16,
-                  cbase + c * 64);
-            dma1(mine + NT * 1024 + n * 256, (uint32_t)nrow[n] * (uint32_t)(a.K / 32) + byte,
-                 sbase + c * 4);
+        for (int n = 0; n < NT; ++n)
+            dma16(mine + n * 1024, c_off[n] + piece * 16, cbase + c * 64);
+#pragma unroll
+        for (int o = 0; o < S::kScaleOps; ++o) {
+            if constexpr (DW) dma4(mine + NT * 1024 + o * 256, s_off[o], sbase + c * 4);
+            else dma1(mine + NT * 1024 + o * 256, s_off[o] + byte, sbase + c * 4);
         }
     };
 
@@ -227,8 +257,14 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 q[n] = *reinterpret_cast<const u32x4*>(ws + n * 1024 + lr * 64 + (g ^ (lr >> 2)) * 16);
-                uint32_t e = *reinterpret_cast<const uint32_t*>(ws + NT * 1024 + n * 256 + lr * 16 + g * 4);
-                e = some ? e & 255 : 0;
+                uint32_t e;
+                if constexpr (DW) {
+                    e = *reinterpret_cast<const uint32_t*>(ws + NT * 1024 + (n * 16 + lr) * 4);
+                    e = e >> (8 * g) & 255;
+                } else {
+                    e = *reinterpret_cast<const uint32_t*>(ws + NT * 1024 + n * 256 + lr * 16 + g * 4);
+                    e = some ? e & 255 : 0;
+                }
                 nan[n] |= e == 255;
                 sc[n] = __uint_as_float(e << 23);
             }
@@ -250,20 +286,8 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
         slot = slot == S::kStages - 1 ? 0 : slot + 1;
     }
 
-    // a NaN scale makes its column NaN
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        uint64_t m = __ballot(nan[n]);
-        if (m) {
-            m |= m >> 32;
-            m |= m >> 16;
-#pragma unroll
-            for (int t = 0; t < TT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (m >> (4 * g + i) & 1) acc[t][n][i] = __uint_as_float(0x7fc00000u);
-        }
-    }
+    for (int n = 0; n < NT; ++n) spoil(acc, n, nan[n], g);
     if constexpr (KW == 1) {
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
@@ -291,6 +315,207 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
     }
 }
 
+// x stationary: the eight waves of a workgroup split K, each keeps its share of x
+// (TT 16-token tiles, CS chunks) in registers for the whole call, and the
+// workgroup walks 16-column tiles.  It reads a tile's rows whole, 16 KB in one
+// piece at K = 2048, where the ring above reads 64 bytes of many rows at a time
+// (which the memory serves at 4 TB/s at most); a tile's partial sums join in LDS.
+// DW: scales in dwords (K a multiple of 128 and scales 4-byte aligned).
+template <int TT, int CS, int NT, bool DW>
+struct MxStill {
+    static constexpr int kCodeOps = NT * CS;
+    static constexpr int kScaleOps = DW ? (kCodeOps + 3) / 4 : kCodeOps;
+    static constexpr int kUnit = kCodeOps * 1024 + kScaleOps * 256;   // a wave's codes and scales
+    static constexpr int kPart = kWaves * TT * NT * 1024;             // the partial sums, twice
+    static constexpr int kFit = (kLdsBytes - 2 * kPart) / (kWaves * kUnit);
+    static constexpr int kStages = kFit > 6 ? 6 : kFit;
+    static constexpr int kOps = kCodeOps + kScaleOps;
+    static_assert(kStages >= 2 && kStages * kOps < 64 && TT <= 2 && NT * TT <= kWaves &&
+                  (CS == 2 || CS == 4));
+};
+
+template <int TT, int CS, int NT, bool DW>
+__global__ void __launch_bounds__(kMxThreads)
+mx4_still_kernel(MxArgs a, PackView pv, int n_units, int log_run) {
+    using S = MxStill<TT, CS, NT, DW>;
+    __shared__ __attribute__((aligned(16))) unsigned char
+        lds[2 * S::kPart + S::kStages * kWaves * S::kUnit];
+    const int walker = blockIdx.x, n_walkers = gridDim.x;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint64_t live, none;
+    live_rows(pv, 0, a.row_cap, live, none, TT * 16);
+    if (!live) return;   // uniform over the workgroup
+    const int lr = lane & 15, g = lane >> 4;
+    const int C = (a.K + 127) / 128;
+    const int c0 = wave * CS;
+
+    // ---- loads: lane l of op o has 16-byte piece i % (4 CS) of row i / (4 CS),
+    // i = 64 o + l, turned by the row so that 16 rows' reads cover all banks
+    constexpr int P = 4 * CS;
+    auto turn = [](int r) { return CS == 2 ? r >> 1 : r; };
+    int crow[S::kCodeOps], coff[S::kCodeOps], srow[S::kScaleOps], soff[S::kScaleOps];
+#pragma unroll
+    for (int o = 0; o < S::kCodeOps; ++o) {
+        const int i = o * 64 + lane;
+        const int piece = (i % P) ^ (turn(i / P) % P);
+        crow[o] = i / P;
+        // a piece past K reads the row's first one in its place
+        coff[o] = (c0 * 4 + piece) * 32 < a.K ? (c0 * 4 + piece) * 16 : 0;
+    }
+#pragma unroll
+    for (int o = 0; o < S::kScaleOps; ++o) {
+        const int i = o * 64 + lane;
+        srow[o] = (DW ? i / CS : i / P) % (NT * 16);
+        const int group = DW ? (c0 + i % CS) * 4 : c0 * 4 + i % P;
+        soff[o] = group * 32 < a.K ? group : 0;
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[2 * S::kPart];
+    auto issue = [&](int u, int slot) {
+        const int n0 = u * (NT * 16);
+        const uint8_t* cbase = a.codes + (size_t)n0 * (a.K / 2);
+        const uint8_t* sbase = a.scales + (size_t)n0 * (a.K / 32);
+        const uint32_t at = lds0 + (slot * kWaves + wave) * S::kUnit;
+        const int last = a.N - 1 - n0;
+#pragma unroll
+        for (int o = 0; o < S::kCodeOps; ++o)
+            dma16(at + o * 1024, (uint32_t)(min(crow[o], last) * (a.K / 2) + coff[o]), cbase);
+#pragma unroll
+        for (int o = 0; o < S::kScaleOps; ++o) {
+            const uint32_t off = (uint32_t)(min(srow[o], last) * (a.K / 32) + soff[o]);
+            if constexpr (DW) dma4(at + S::kCodeOps * 1024 + o * 256, off, sbase);
+            else dma1(at + S::kCodeOps * 1024 + o * 256, off, sbase);
+        }
+    };
+
+    // ---- the wave's share of x: lane group g is to hold elements 32 g .. of each
+    // chunk, which a lane's own loads would fetch as 64 scattered pieces each.  Load j
+    // takes the 64 bytes 32 j .. of a row by its four lanes instead, and the 4 x 4
+    // transposition between loads and lane groups is two rounds of lane swaps.
+    bf16x8 xf[TT][CS][4];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        const uint16_t* xr = a.x + (size_t)min(t * 16 + lr, a.row_cap - 1) * a.K;
+#pragma unroll
+        for (int c = 0; c < CS; ++c) {
+            u32x4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = (c0 + c) * 128 + j * 32;
+                v[j] = u32x4{0, 0, 0, 0};
+                if (k < a.K) v[j] = *reinterpret_cast<const u32x4*>(xr + k + g * 8);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32x2 p = __builtin_amdgcn_permlane32_swap(v[0][i], v[2][i], false, false);
+                const u32x2 q = __builtin_amdgcn_permlane32_swap(v[1][i], v[3][i], false, false);
+                const u32x2 l = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false);
+                const u32x2 h = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
+                v[0][i] = l[0], v[1][i] = l[1], v[2][i] = h[0], v[3][i] = h[1];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xf[t][c][j] = __builtin_bit_cast(bf16x8, v[j]);
+        }
+    }
+
+    // The compiler has to know that x is there: left to itself it waits for x inside
+    // the loop, and so for every load of the ring, at each tile.
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    asm volatile("" ::: "memory");
+
+    // the workgroup's units: runs of 2^log_run neighbours, every n_walkers-th run
+    const int runs = (n_units + (1 << log_run) - 1) >> log_run;
+    int walk = runs > walker ? ((runs - walker + n_walkers - 1) / n_walkers) << log_run : 0;
+    if (walk && (runs - 1) % n_walkers == walker) walk -= (runs << log_run) - n_units;
+    auto unit = [&](int s) {
+        return ((walker + (s >> log_run) * n_walkers) << log_run) + (s & ((1 << log_run) - 1));
+    };
+    // codes and scales of a unit, from its slot to registers
+    u32x4 q[NT][CS];
+    uint32_t e[NT][CS];
+    auto fetch = [&](int slot) {
+        const unsigned char* in = lds + 2 * S::kPart + (slot * kWaves + wave) * S::kUnit;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < CS; ++c) {
+                const int r = n * 16 + lr;
+                q[n][c] = *reinterpret_cast<const u32x4*>(
+                    in + r * (CS * 64) + ((c * 4 + g) ^ (turn(r) % P)) * 16);
+                e[n][c] = *reinterpret_cast<const uint32_t*>(
+                    in + S::kCodeOps * 1024 + (DW ? r * CS + c : r * P + c * 4 + g) * 4);
+            }
+    };
+#pragma unroll
+    for (int s = 0; s < S::kStages; ++s)
+        if (s < walk) issue(unit(s), s);
+    if (S::kStages <= walk)
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S::kStages - 1) * S::kOps) : "memory");
+    else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (walk) fetch(0);
+    int slot = 0;
+    for (int s = 0; s < walk; ++s) {
+        const int n0 = unit(s) * (NT * 16);
+        // the unit is in registers and its slot free (this wave alone reads it)
+        if (s == 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (s + S::kStages < walk) issue(unit(s + S::kStages), slot);
+        slot = slot == S::kStages - 1 ? 0 : slot + 1;
+        f32x4 acc[TT][NT];
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        bool nan[NT] = {};
+#pragma unroll
+        for (int c = 0; c < CS; ++c) {
+            float sc[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                uint32_t ee = DW ? e[n][c] >> (8 * g) : e[n][c];
+                ee = ((c0 + c) * 4 + g) * 32 < a.K ? ee & 255 : 0;
+                nan[n] |= ee == 255;
+                sc[n] = __uint_as_float(ee << 23);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const bf16x8 w = weights8(q[n][c][j], sc[n]);
+#pragma unroll
+                    for (int t = 0; t < TT; ++t)
+                        acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xf[t][c][j],
+                                                                            acc[t][n], 0, 0, 0);
+                }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) spoil(acc, n, nan[n], g);
+        // behind the wait the next unit's codes and scales have landed
+        if (s + 1 < walk) {
+            if (s + S::kStages < walk)
+                asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S::kStages - 1) * S::kOps) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            fetch(slot);
+        }
+        f32x4* part = reinterpret_cast<f32x4*>(lds + (s & 1) * S::kPart);
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) part[((wave * TT + t) * NT + n) * 64 + lane] = acc[t][n];
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        // joined in order; the next partials go to the other half, and the barrier
+        // after that lies between this read and the next write here
+        if (wave < TT * NT) {
+            f32x4 v = part[wave * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v += part[(w * TT * NT + wave) * 64 + lane];
+            const int t = wave / NT, n = wave % NT;
+            if (live >> (t * 16 + lr) & 1) store4(a, t * 16 + lr, n0 + n * 16 + g * 4, v);
+        }
+    }
+}
+
 }  // namespace
 
 hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scales, int N, int K,
@@ -302,30 +527,65 @@ hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scale
              static_cast<const uint8_t*>(scales), y, N, K, cap, y_dtype == FB_BF16 ? 1 : 0, 0};
     a.vec_out = N % 4 == 0 && ((uintptr_t)y & (y_dtype == FB_BF16 ? 7 : 15)) == 0;
     const int tiles = (N + 15) / 16;
+    const bool dw = K % 128 == 0 && ((uintptr_t)scales & 3) == 0;
     auto launch = [&](auto tt, auto nt, auto kw) {
         constexpr int T = decltype(tt)::value, M = decltype(nt)::value, W = decltype(kw)::value;
         const int per = kWaves / W * M;
         const int groups = (tiles + per - 1) / per;
         const int rg = (cap + T * 16 - 1) / (T * 16);
-        hipLaunchKernelGGL((mx4_kernel<T, M, W>), dim3((unsigned)groups * rg), dim3(kMxThreads), 0,
-                           stream, a, pv, groups);
+        void (*kernel)(MxArgs, PackView, int) =
+            dw ? mx4_kernel<T, M, W, true> : mx4_kernel<T, M, W, false>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups * rg), dim3(kMxThreads), 0, stream, a, pv,
+                           groups);
     };
     using std::integral_constant;
 #define FB_C(n) integral_constant<int, n>()
     const int rows16 = (cap + 15) / 16;
-    // few columns: split K until every CU has a workgroup
+    // x stationary: long outputs (16 tiles a CU), where the time to fetch x is small
+    // beside the walk, K from 12 chunks to what the registers hold, 32 rows at most.
+    // M x N x K, this form and the ring: 1 x 131072 x 4096 56 and 105 us, 32 x 131072 x
+    // 4096 65 and 109; 1 x 65536 x 1536 14.3 and 15.4, 32 x 65536 x 1536 17.7 and 17.0.
+    // Outside: 1 x 16384 x 2048 7.3 and 6.3, 32 x 131072 x 1152 27.9 and 23.3, 64 x
+    // 157184 x 2048 56 and 58.
+    const int C = (K + 127) / 128;
+    if (C >= 12 && C <= 32 && rows16 <= 2 && tiles >= 16 * cu_count) {
+        auto still = [&](auto t, auto c, auto n) {
+            constexpr int T = decltype(t)::value, S = decltype(c)::value, M = decltype(n)::value;
+            // runs of four tiles, 128 bytes of a row of bf16 results: written by one
+            // workgroup, they leave its L2 as whole lines; unless the runs leave the
+            // longest walk a tenth longer
+            const int units = (tiles + M - 1) / M, log_run = M == 1 ? 2 : 1;
+            const int longest = ((((units - 1) >> log_run) + cu_count) / cu_count) << log_run;
+            const bool run = longest * 10 <= (units + cu_count - 1) / cu_count * 11;
+            void (*kernel)(MxArgs, PackView, int, int) =
+                dw ? mx4_still_kernel<T, S, M, true> : mx4_still_kernel<T, S, M, false>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)cu_count), dim3(kMxThreads), 0, stream, a, pv,
+                               units, run ? log_run : 0);
+        };
+        if (C <= 16) {
+            if (rows16 == 1) still(FB_C(1), FB_C(2), FB_C(2));
+            else still(FB_C(2), FB_C(2), FB_C(2));
+        } else {
+            if (rows16 == 1) still(FB_C(1), FB_C(4), FB_C(1));
+            else still(FB_C(2), FB_C(4), FB_C(1));
+        }
+        return hipGetLastError();
+    }
+    // few columns: split K while the waves of a workgroup a CU are not all busy
     const int TT = rows16 <= 1 ? 1 : rows16 <= 2 ? 2 : rows16 <= 4 ? 4 : rows16 <= 6 ? 6 : 8;
     auto units = [&](int tt) { return (long long)tiles * ((rows16 + tt - 1) / tt); };
     const long long want = 8LL * cu_count;     // one tile per wave
     if (units(TT) <= want / 2) {
         const int t = TT > 4 ? 4 : TT;
-        if (units(t) <= want / 8 && t == 1) launch(FB_C(1), FB_C(1), FB_C(8));
-        else if (units(t) <= want / 8 && t == 2) launch(FB_C(2), FB_C(1), FB_C(8));
-        else if (units(t) <= want / 4 || t < 4) {
-            if (t == 1) launch(FB_C(1), FB_C(1), FB_C(4));
-            else if (t == 2) launch(FB_C(2), FB_C(1), FB_C(4));
-            else launch(FB_C(4), FB_C(1), FB_C(4));
-        } else launch(FB_C(4), FB_C(1), FB_C(2));
+        auto split = [&](auto tt) {
+            if (units(t) <= want / 8 && t < 4) {
+                if constexpr (decltype(tt)::value < 4) launch(tt, FB_C(1), FB_C(8));
+            } else if (units(t) <= want / 4) launch(tt, FB_C(1), FB_C(4));
+            else launch(tt, FB_C(1), FB_C(2));
+        };
+        if (t == 1) split(FB_C(1));
+        else if (t == 2) split(FB_C(2));
+        else split(FB_C(4));
         return hipGetLastError();
     }
     // tiles per wave: the least (rounds of workgroups) x (tiles + a start)

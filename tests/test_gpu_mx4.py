@@ -122,3 +122,91 @@ def test_large_vocabulary():
         y = torch.full((bt.row_cap, N), 5.0, device="cuda")
         fb.fb_mx4_linear(x, codes, scales, bt.pack, y)
         check(bt, codes[pick].cpu().numpy(), scales[pick].cpu().numpy(), x.cpu(), y[:, pick], "f32")
+
+
+# ---- long outputs: the same check on the device, in float64 ---------------------
+TABLE = [tail.e2m1(c) for c in range(16)]
+
+
+def check_device(bt, codes, scales, x, y, out):
+    """check() with the float64 work on the device, 8192 columns at a time."""
+    live, K = torch.from_numpy(bt.live).cuda(), x.shape[1]
+    table = torch.tensor(TABLE, dtype=torch.float64, device="cuda")
+    xs = x.double()[live]
+    gamma = K * 2.0 ** -24 / (1 - K * 2.0 ** -24)
+    for n in range(0, codes.shape[0], 8192):
+        c, s = codes[n:n + 8192].int(), scales[n:n + 8192].double()
+        w = torch.stack((table[c & 15], table[c >> 4]), dim=2).flatten(1)
+        w *= torch.exp2(s - 127).repeat_interleave(32, dim=1)
+        exact = xs @ w.t().contiguous()
+        tol = gamma * (xs.abs() @ w.abs().t().contiguous()) + HALF_STEP[out] * exact.abs()
+        assert torch.all((y[live, n:n + 8192].double() - exact).abs() <= tol)
+    dead = torch.ones(bt.row_cap, dtype=torch.bool)
+    dead[bt.live] = False
+    assert torch.all(y[dead.cuda()] == 5)
+
+
+def long_inputs(bt, N, K, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(118, 130, (N, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+    x = torch.randn(bt.row_cap, K, generator=g, device="cuda").to(torch.bfloat16)
+    return codes, scales, x
+
+
+def long_call(bt, codes, scales, x, out):
+    y = torch.full((bt.row_cap, codes.shape[0]), 5.0, dtype=TORCH[out], device="cuda")
+    fb.fb_mx4_linear(x, codes, scales, bt.pack, y)
+    return y
+
+
+@pytest.mark.parametrize("rows", [1, 16, 19, 32, 50])
+@pytest.mark.parametrize("N,K", [(8193, 160), (8208, 2080), (12300, 1056), (16400, 1024),
+                                 (65521, 2016), (65536, 1536), (65603, 2048), (66001, 2080),
+                                 (69700, 4096), (70017, 3904), (65552, 1408), (65552, 4128)])
+def test_long_outputs(rows, N, K):
+    bt = Batch(w=[1], o=[3], bl=rows, W_max=1).cuda()
+    case = long_inputs(bt, N, K, seed=rows + K)
+    out = "bf16" if rows % 16 else "f32"
+    check_device(bt, *case, long_call(bt, *case, out), out)
+
+
+@pytest.mark.parametrize("N", [9000, 65557])
+@pytest.mark.parametrize("K", [2016, 4096])
+def test_long_outputs_padded(N, K):
+    """Dead rows between live ones, their contents NaN; an infinite row; a NaN scale."""
+    bt = Batch(w=[1, 3, 2], o=[12, 7, 33], bl=3, W_max=3, layout="padded", inactive=(1,)).cuda()
+    codes, scales, x = long_inputs(bt, N, K, seed=4)
+    y = long_call(bt, codes, scales, x, "f32")
+    check_device(bt, codes, scales, x, y, "f32")
+    dead = torch.ones(bt.row_cap, dtype=torch.bool)
+    dead[bt.live] = False
+    x[dead.cuda()] = float("nan")
+    x[int(bt.live[0])] = float("inf")
+    scales[[7, N - 1], K // 32 - 1] = 255
+    z = long_call(bt, codes, scales, x, "f32")
+    assert torch.isnan(z[bt.live][:, [7, N - 1]]).all()
+    others = torch.ones(N, dtype=torch.bool, device="cuda")
+    others[[7, N - 1]] = False
+    rest = bt.live[1:]
+    assert torch.equal(z[rest][:, others], y[rest][:, others])
+
+
+@pytest.mark.parametrize("N,K", [(96, 512), (8208, 1024), (65552, 2048), (65552, 4096)])
+def test_scales_at_any_byte(N, K):
+    """The same bits whatever the address of the scales."""
+    bt = Batch(**BATCHES["ragged"]).cuda()
+    codes, scales, x = long_inputs(bt, N, K, seed=2)
+    y = long_call(bt, codes, scales, x, "f32")
+    check_device(bt, codes, scales, x, y, "f32")
+    raw = torch.zeros(scales.numel() + 8, dtype=torch.uint8, device="cuda")
+    for at in (1, 2, 3):
+        s = raw[at:at + scales.numel()].view(*scales.shape)
+        s.copy_(scales)
+        assert torch.equal(y, long_call(bt, codes, s, x, "f32"))
+
+
+def test_long_output_nothing_live():
+    bt = Batch(**BATCHES["nothing"]).cuda()
+    case = long_inputs(bt, 65552, 1536)
+    assert torch.all(long_call(bt, *case, "f32") == 5)
