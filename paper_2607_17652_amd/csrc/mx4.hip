@@ -581,16 +581,37 @@ hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scale
     auto units = [&](int tt) { return (long long)tiles * ((rows16 + tt - 1) / tt); };
     const long long want = 8LL * cu_count;     // one tile per wave
     if (units(TT) <= want / 2) {
-        const int t = TT > 4 ? 4 : TT;
+        // the cheapest of T token tiles and KW waves to a tile: rounds of workgroups x
+        // (a start + stages x a stage's time, us, fitted to what all eight pairs take:
+        // 0.43 at (1, 2) to 1.1 at (4, 4)).  32 x 4096 x 4096: (1, 4) 6.3 us, (2, 8)
+        // 7.4, (4, 2) 15.6; 64 x 4096 x 4096: (2, 4) 8.0, (1, 2) 9.1, (4, 4) 11.0;
+        // 96 x 8192 x 4096: (4, 2) 16.6, (1, 2) 18.2, (2, 2) 21.0.
+        int t = 1, kw = 2;
+        double best = 1e30;
+        for (int T : {1, 2, 4, 6, 8})
+            for (int W = 2; W <= kWaves && W * T <= 16; W *= 2) {
+                const long long groups =
+                    (long long)((tiles * W + 7) / 8) * ((rows16 + T - 1) / T);
+                const double cost = (double)((groups + cu_count - 1) / cu_count) *
+                                    (2.5 + (C + W - 1) / W * (0.3 + 0.045 * T + 0.04 * T * W));
+                if (cost < best) {
+                    best = cost;
+                    t = T;
+                    kw = W;
+                }
+            }
         auto split = [&](auto tt) {
-            if (units(t) <= want / 8 && t < 4) {
-                if constexpr (decltype(tt)::value < 4) launch(tt, FB_C(1), FB_C(8));
-            } else if (units(t) <= want / 4) launch(tt, FB_C(1), FB_C(4));
-            else launch(tt, FB_C(1), FB_C(2));
+            if (kw == 2) launch(tt, FB_C(1), FB_C(2));
+            else if constexpr (decltype(tt)::value <= 4) {
+                if (kw == 4) launch(tt, FB_C(1), FB_C(4));
+                else if constexpr (decltype(tt)::value <= 2) launch(tt, FB_C(1), FB_C(8));
+            }
         };
         if (t == 1) split(FB_C(1));
         else if (t == 2) split(FB_C(2));
-        else split(FB_C(4));
+        else if (t == 4) split(FB_C(4));
+        else if (t == 6) split(FB_C(6));
+        else split(FB_C(8));
         return hipGetLastError();
     }
     // tiles per wave: the least (rounds of workgroups) x (tiles + a start)

@@ -171,6 +171,15 @@ def test_long_outputs(rows, N, K):
     check_device(bt, *case, long_call(bt, *case, out), out)
 
 
+@pytest.mark.parametrize("rows", [70, 96, 127, 200, 512])
+@pytest.mark.parametrize("N,K", [(1030, 4128), (2048, 2048), (8208, 1056), (16384, 1024)])
+def test_many_rows(rows, N, K):
+    bt = Batch(w=[1], o=[3], bl=rows, W_max=1).cuda()
+    case = long_inputs(bt, N, K, seed=rows + K)
+    out = "bf16" if rows % 16 else "f32"
+    check_device(bt, *case, long_call(bt, *case, out), out)
+
+
 @pytest.mark.parametrize("N", [9000, 65557])
 @pytest.mark.parametrize("K", [2016, 4096])
 def test_long_outputs_padded(N, K):
