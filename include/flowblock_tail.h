@@ -78,7 +78,7 @@ int fb_residual_norm(const void* y, const void* h, const void* gate,
  *           2i + 1 in the high half; 16-byte aligned
  *   scales  uint8 [N][K/32] (E8M0)
  *   y       [row_cap][N], y_dtype FB_BF16 or FB_F32; not x
- *   N >= 1; K a positive multiple of 32, at most 65536
+ *   N 1 .. 2^30; K a positive multiple of 32, at most 65536
  * Scales: 2 .. 252 keep every weight normal in bf16; below, weights under
  * 2^-126 may be taken as 0; above, weights past bf16's largest are infinite;
  * 255 (E8M0's NaN) makes its 32 weights NaN.
@@ -91,9 +91,9 @@ int fb_mx4_linear(const void* x, const void* codes, const void* scales, int N,
 
 /* Penalties of one request (device array [B]).  16 bytes. */
 typedef struct fb_rule_params {
-    float   repetition;   /* r > 0; 1 is none                                 */
-    float   presence;     /* p; 0 is none                                     */
-    float   frequency;    /* f; 0 is none                                     */
+    float   repetition;   /* r, 2^-40 .. 2^40; 1 is none                      */
+    float   presence;     /* p, finite; 0 is none                             */
+    float   frequency;    /* f, finite; 0 is none                             */
     int32_t reserved;
 } fb_rule_params;
 

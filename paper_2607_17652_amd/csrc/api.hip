@@ -578,6 +578,7 @@ int fb_mx4_linear(const void* x, const void* codes, const void* scales, int N, i
     int rc = check_pack(pack);
     if (rc) return rc;
     if (N < 1) return fail(FB_E_INVAL, "N must be >= 1");
+    if (N > 1 << 30) return fail(FB_E_UNSUPPORTED, "N %d above 2^30", N);
     if (K < 32 || K % 32) return fail(FB_E_INVAL, "K %d must be a positive multiple of 32", K);
     if (K > 65536) return fail(FB_E_UNSUPPORTED, "K %d above 65536", K);
     if (y_dtype != FB_BF16 && y_dtype != FB_F32)

@@ -135,7 +135,8 @@ rules_build_kernel(fb_logit_rules rules, const fb_req_state* __restrict__ st,
     bool bad = false;
     if (rules.params) {
         p = rules.params[b];
-        bad = !(p.repetition > 0.f) || !finite(p.repetition) || !finite(p.presence) ||
+        // a range in which r and 1 / r are normal, for the quotient of adjust()
+        bad = !(p.repetition >= 0x1p-40f && p.repetition <= 0x1p40f) || !finite(p.presence) ||
               !finite(p.frequency);
     }
     int lo = 0, hi = 0;
@@ -266,11 +267,12 @@ rules_build_kernel(fb_logit_rules rules, const fb_req_state* __restrict__ st,
 
 // z' of a touched token.  z / r is the correctly rounded quotient: z times the
 // rounded reciprocal, corrected once by its exact remainder (Markstein, "Computation
-// of elementary functions on the IBM RISC System/6000 processor", 1990).
+// of elementary functions on the IBM RISC System/6000 processor", 1990).  Past the
+// type's range it is the infinity that the product is.
 __device__ inline float adjust(float z, const uint2& adj, const float2& rec) {
 #pragma clang fp contract(off)
     const float q = z * rec.y;
-    const float div = fmaf(fmaf(-q, rec.x, z), rec.y, q);
+    const float div = finite(q) ? fmaf(fmaf(-q, rec.x, z), rec.y, q) : q;
     const float pen = z > 0.f ? div : z * rec.x;
     return (adj.y & kSeen ? pen : z) + __uint_as_float(adj.x);
 }

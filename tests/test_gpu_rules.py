@@ -338,3 +338,31 @@ def test_update_under_rules_is_the_update_on_adjusted_logits(force):
     for k in ("L", "R", "active"):
         assert np.array_equal(st[k], o["state"][k])
     assert np.all(bt.tok.cpu().numpy()[1, 8:12] == mask_id)
+
+
+@pytest.mark.parametrize("r", [2.0 ** -41, 2.0 ** 41, np.inf])
+def test_repetition_out_of_range(r):
+    bt = Batch(**BATCHES["ragged"], V=300).cuda()
+    rules = Rules(bt, 300, seed=3, n_bias=None, n_masks=0)
+    rules.params[1, 0] = r
+    run = Run(bt, 300, "f32", rules, logits(bt, 300, "f32")).go()
+    s = fb.fb_pack_read_status(bt.pack)
+    assert (s["code"], s["request"]) == (fb.FB_DERR_RULE, 1)
+    assert torch.all(run.argmax[bt.live[bt.row_req[bt.live] == 1]] == -1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("r", [2.0 ** -40, 1.3e-12, 7.7e11, 2.0 ** 40])
+def test_written_logits_of_any_size(r, dtype):
+    """Quotients and products past the type's range are its infinities."""
+    V = 500
+    bt = Batch(**BATCHES["ragged"], V=V).cuda()
+    rules = Rules(bt, V, seed=3)
+    rules.params[:, 0] = r
+    rng = np.random.default_rng(0)
+    size = 2.0 ** rng.integers(-20, 127, size=(bt.row_cap, V))
+    z = torch.from_numpy(rng.uniform(1, 2, size.shape) * size * rng.choice([-1, 1], size.shape)) \
+        .to(TORCH[dtype]).cuda()
+    run = Run(bt, V, dtype, rules, z).go()
+    want = rules.rows(bt, V, z.float().cpu().numpy()[bt.live])
+    assert torch.equal(run.out.float().cpu()[bt.live], torch.from_numpy(want).to(TORCH[dtype]).float())

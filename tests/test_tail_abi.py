@@ -87,7 +87,8 @@ def test_residual_norm_refuses(lib, pack, want, change):
 @pytest.mark.parametrize("want,change", [
     ("INVAL", dict(x=None)), ("INVAL", dict(codes=None)), ("INVAL", dict(scales=None)),
     ("INVAL", dict(y=None)), ("INVAL", dict(N=0)), ("INVAL", dict(K=0)), ("INVAL", dict(K=48)),
-    ("UNSUPPORTED", dict(K=65568)), ("UNSUPPORTED", dict(dtype=3)), ("INVAL", dict(x=OFF8)),
+    ("UNSUPPORTED", dict(K=65568)), ("UNSUPPORTED", dict(N=(1 << 30) + 1)),
+    ("UNSUPPORTED", dict(dtype=3)), ("INVAL", dict(x=OFF8)),
     ("INVAL", dict(codes=OFF8)), ("INVAL", dict(y=ODD)), ("INVAL", dict(y=P)),
     ("INVAL", dict(pack=None)),
 ])
