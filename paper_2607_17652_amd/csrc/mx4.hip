@@ -131,6 +131,13 @@ __device__ inline void spoil(f32x4 (&acc)[TT][NT], int n, bool nan, int g) {
             if (m >> (4 * g + i) & 1) acc[t][n][i] = __uint_as_float(0x7fc00000u);
 }
 
+// Where row r of 16 has its 16-byte piece p in LDS: at p ^ turn.  A 16-byte read of a
+// wave goes in four steps of sixteen lanes, among them lanes 0-3, 12-15 and 20-27: two
+// lane groups g with eight rows each, whose pieces must not share a bank.  (Turned by
+// the row itself, half of the x reads met a conflict: 1024 x 16384 x 4096 107 us.)
+__device__ inline int turn_x(int r) { return r ^ ((r ^ r >> 1) & 4); }   // rows of 256 bytes
+__device__ inline int turn_w(int r) { return r & 4 ? 3 : 0; }            // rows of 64 bytes
+
 // TT 16-token tiles, NT 16-column tiles a wave, KW waves to a tile.
 // DW: whole chunks (K a multiple of 128) and scales 4-byte aligned, so that a row's
 // four scales of a chunk are one dword; a byte a lane otherwise.
@@ -169,10 +176,9 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
     const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0];
 
     // ---- loads ---------------------------------------------------------------
-    // codes: four neighbouring lanes take one row's 64 bytes of a chunk, the
-    // 16-byte pieces turned by row / 4 so that the 16 rows of a read cover all
-    // banks.  x: sixteen lanes take one row's 256 bytes, turned by the row.
-    const int wr = lane >> 2, wp = (lane & 3) ^ (wr >> 2);
+    // codes: four neighbouring lanes take one row's 64 bytes of a chunk.  x: sixteen
+    // lanes take one row's 256 bytes.  Their 16-byte pieces are turned by the row.
+    const int wr = lane >> 2, wp = (lane & 3) ^ turn_w(wr);
     const int nb = min(n0, a.N - 1);
     const uint8_t* cbase = a.codes + (size_t)nb * (a.K / 2);
     const uint8_t* sbase = a.scales + (size_t)nb * (a.K / 32);
@@ -194,7 +200,7 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
         const int r = (o % (TT * 4)) * 4 + (lane >> 4);
         x_cc[i] = o / (TT * 4);
         x_off[i] = (uint32_t)min(r, a.row_cap - 1 - r0) * (uint32_t)a.K * 2 +
-                   ((lane & 15) ^ (r & 15)) * 16;
+                   ((lane & 15) ^ turn_x(r & 15)) * 16;
     }
     auto issue = [&](int s, int slot) {
         const uint32_t at = lds0 + slot * S::kStage;
@@ -206,7 +212,7 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
                 dma16(at + o * 1024, x_off[i], xbase + c * 128);
             } else {
                 const int r = (o % (TT * 4)) * 4 + (lane >> 4);
-                const int k = c * 128 + ((lane & 15) ^ (r & 15)) * 8;
+                const int k = c * 128 + ((lane & 15) ^ turn_x(r & 15)) * 8;
                 const void* p = k < a.K
                     ? static_cast<const void*>(reinterpret_cast<const char*>(xbase + c * 128) + x_off[i])
                     : static_cast<const void*>(mx4_zeros);
@@ -260,7 +266,7 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
             const bool some = (4 * c + g) * 32 < a.K;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                q[n] = *reinterpret_cast<const u32x4*>(ws + n * 1024 + lr * 64 + (g ^ (lr >> 2)) * 16);
+                q[n] = *reinterpret_cast<const u32x4*>(ws + n * 1024 + lr * 64 + (g ^ turn_w(lr)) * 16);
                 uint32_t e;
                 if constexpr (DW) {
                     e = *reinterpret_cast<const uint32_t*>(ws + NT * 1024 + (n * 16 + lr) * 4);
@@ -280,7 +286,7 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
 #pragma unroll
                 for (int t = 0; t < TT; ++t) {
                     const bf16x8 b = *reinterpret_cast<const bf16x8*>(
-                        xs + (t * 16 + lr) * 256 + ((g * 4 + j) ^ lr) * 16);
+                        xs + (t * 16 + lr) * 256 + ((g * 4 + j) ^ turn_x(lr)) * 16);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
                         acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], b, acc[t][n], 0, 0, 0);
