@@ -15,7 +15,7 @@
 //             16-column tiles; where the columns are few, KW waves share a
 //             tile, take the chunks of a stage in turn and join at the end.
 //             Many rows are bound by the matrix cores: 1024 x 16384 x 4096 107 us,
-//             1.28 PFLOP/s; 96 x 157184 x 2048 67 us, 0.92 PFLOP/s; 1 x 4096 x
+//             1.29 PFLOP/s; 96 x 157184 x 2048 68 us, 0.91 PFLOP/s; 1 x 4096 x
 //             4096 5.1 us.  A large bf16 product reaches 1.13 PFLOP/s on this card.
 // mx4_still_kernel  few rows and a long output: x stays in registers and the
 //             weights of whole rows stream by.
@@ -132,9 +132,9 @@ __device__ inline void spoil(f32x4 (&acc)[TT][NT], int n, bool nan, int g) {
 }
 
 // Where row r of 16 has its 16-byte piece p in LDS: at p ^ turn.  A 16-byte read of a
-// wave goes in four steps of sixteen lanes, among them lanes 0-3, 12-15 and 20-27: two
-// lane groups g with eight rows each, whose pieces must not share a bank.  (Turned by
-// the row itself, half of the x reads met a conflict: 1024 x 16384 x 4096 107 us.)
+// wave goes in four steps of sixteen lanes, one of them lanes 0-3, 12-15 and 20-27: two
+// lane groups g with eight rows each, whose pieces must not share a bank.  Turned by
+// the row itself they did, for 12-17% of the cycles: 1024 x 4096 x 4096 49 us, 43 so.
 __device__ inline int turn_x(int r) { return r ^ ((r ^ r >> 1) & 4); }   // rows of 256 bytes
 __device__ inline int turn_w(int r) { return r & 4 ? 3 : 0; }            // rows of 64 bytes
 
