@@ -61,7 +61,7 @@ __device__ inline float addend(float bias, uint32_t c, const fb_rule_params& p) 
 
 // Barrier behind which the workgroup sees its own stores to memory, and its
 // atomics come after them.  (A device-wide fence would write the L2 back: the
-// build of 256 requests took 160 us with two of them, 12 with this.)
+// build of 256 requests took 160 us with two of them, 15 with this.)
 __device__ inline void workgroup_sync() {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
