@@ -17,6 +17,7 @@
 //             Many rows are bound by the matrix cores: 1024 x 16384 x 4096 107 us,
 //             1.29 PFLOP/s; 96 x 157184 x 2048 68 us, 0.91 PFLOP/s; 1 x 4096 x
 //             4096 5.1 us.  A large bf16 product reaches 1.13 PFLOP/s on this card.
+// mx4_pair_kernel  more rows and a long output: codes two chunks at a time.
 // mx4_still_kernel  few rows and a long output: x stays in registers and the
 //             weights of whole rows stream by.
 #include <type_traits>
@@ -325,6 +326,149 @@ mx4_kernel(MxArgs a, PackView pv, int n_groups) {
     }
 }
 
+// Long outputs: as the ring, but a wave reads its codes two chunks at a time, 128
+// bytes of a row in one piece (64 bytes are served at 4 TB/s at most).  They go to
+// registers when a pair of chunks begins, and their one slot is filled again while
+// the pair is multiplied; x has a slot for each chunk of the pair.  K is a multiple
+// of 256 and the scales are 4-byte aligned.
+template <int TT, int NT>
+struct MxPair {
+    static constexpr int kX = TT * 4096;                         // x of a chunk
+    static constexpr int kScaleOps = (NT + 1) / 2;
+    static constexpr int kW = NT * 2048 + kScaleOps * 256;       // a wave's codes and scales
+    static constexpr int kXOps = TT / 2;                         // x loads per wave and chunk
+    static constexpr int kWOps = 2 * NT + kScaleOps;
+    static constexpr int kLds = 2 * kX + kWaves * kW;
+    static_assert(TT % 2 == 0 && TT * NT <= 24 && kLds <= kLdsBytes && kWOps < 64);
+};
+
+template <int TT, int NT>
+__global__ void __launch_bounds__(kMxThreads)
+mx4_pair_kernel(MxArgs a, PackView pv, int n_groups) {
+    using S = MxPair<TT, NT>;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[S::kLds];
+    const int ng = blockIdx.x % n_groups;
+    const int r0 = blockIdx.x / n_groups * (TT * 16);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint64_t m0, m1;
+    live_rows(pv, r0, a.row_cap, m0, m1, TT * 16);
+    if (!(m0 | m1)) return;   // uniform over the workgroup
+    const int n0 = (ng * kWaves + wave) * (NT * 16);
+    const int lr = lane & 15, g = lane >> 4;
+    const int pairs = a.K / 256;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0];
+    const uint32_t w_lds = lds0 + 2 * S::kX + wave * S::kW;
+
+    // ---- loads: eight lanes take one row's 128 bytes of codes, two its scales
+    const int nb = min(n0, a.N - 1);
+    const uint8_t* cbase = a.codes + (size_t)nb * (a.K / 2);
+    const uint8_t* sbase = a.scales + (size_t)nb * (a.K / 32);
+    const int last = a.N - 1 - nb;
+    const int wr = lane >> 3;                                // of the 8 rows of a load
+    const int piece = ((lane & 7) ^ (lane >> 4)) * 16;       // turned by the row's half
+    const uint16_t* xbase = a.x + (size_t)r0 * a.K;
+    uint32_t x_off[S::kXOps];
+#pragma unroll
+    for (int i = 0; i < S::kXOps; ++i) {
+        const int row = (wave * S::kXOps + i) * 4 + (lane >> 4);
+        x_off[i] = (uint32_t)min(row, a.row_cap - 1 - r0) * (uint32_t)a.K * 2 +
+                   ((lane & 15) ^ turn_x(row & 15)) * 16;
+    }
+    auto issue_x = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < S::kXOps; ++i)
+            dma16(lds0 + (c & 1) * S::kX + (wave * S::kXOps + i) * 1024, x_off[i], xbase + c * 128);
+    };
+    auto issue_w = [&](int p) {
+#pragma unroll
+        for (int o = 0; o < 2 * NT; ++o)
+            dma16(w_lds + o * 1024,
+                  (uint32_t)(min(o * 8 + wr, last) * (a.K / 2) + (piece ^ (o & 1) * 64)),
+                  cbase + p * 128);
+#pragma unroll
+        for (int o = 0; o < S::kScaleOps; ++o) {
+            const int row = min(min(o * 32 + lane / 2, NT * 16 - 1), last);
+            dma4(w_lds + NT * 2048 + o * 256, (uint32_t)(row * (a.K / 32) + (lane & 1) * 4),
+                 sbase + p * 8);
+        }
+    };
+
+    f32x4 acc[TT][NT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    bool nan[NT] = {};
+    u32x4 q[NT][2];
+    uint32_t e[NT][2];
+    auto multiply = [&](int c) {
+        const unsigned char* xs = lds + c * S::kX;
+        float sc[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t b = e[n][c] >> (8 * g) & 255;
+            nan[n] |= b == 255;
+            sc[n] = __uint_as_float(b << 23);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bf16x8 w[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) w[n] = weights8(q[n][c][j], sc[n]);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const bf16x8 b = *reinterpret_cast<const bf16x8*>(
+                    xs + (t * 16 + lr) * 256 + ((g * 4 + j) ^ turn_x(lr)) * 16);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], b, acc[t][n], 0, 0, 0);
+            }
+        }
+    };
+
+    // A barrier a chunk: behind it the chunk's x has landed for every wave, and the
+    // x of the chunk before may be overwritten.
+    issue_x(0);
+    issue_w(0);
+    for (int p = 0; p < pairs; ++p) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        issue_x(2 * p + 1);
+        const unsigned char* ws = lds + 2 * S::kX + wave * S::kW;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                q[n][c] = *reinterpret_cast<const u32x4*>(
+                    ws + (n * 16 + lr) * 128 + ((c * 4 + g) ^ (lr >> 1)) * 16);
+                e[n][c] = *reinterpret_cast<const uint32_t*>(
+                    ws + NT * 2048 + ((n * 16 + lr) * 2 + c) * 4);
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (p + 1 < pairs) issue_w(p + 1);
+        multiply(0);
+        if (p + 1 < pairs) {
+            // x of the second chunk is older than the codes of the next pair
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(S::kWOps) : "memory");
+            issue_x(2 * p + 2);
+        } else {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+        multiply(1);
+    }
+
+#pragma unroll
+    for (int n = 0; n < NT; ++n) spoil(acc, n, nan[n], g);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        const uint64_t m = t < 4 ? m0 >> (16 * t) : m1 >> (16 * (t - 4));
+        if (!(m >> lr & 1)) continue;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            store4(a, r0 + t * 16 + lr, n0 + n * 16 + g * 4, acc[t][n]);
+    }
+}
+
 // x stationary: the eight waves of a workgroup split K, each keeps its share of x
 // (TT 16-token tiles, CS chunks) in registers for the whole call, and the
 // workgroup walks units of NT 16-column tiles.  It reads a tile's rows whole, 16 KB
@@ -630,6 +774,32 @@ hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scale
             best = cost;
             nt = n;
         }
+    }
+    // Codes two chunks at a time, while they and the sums fit the registers (beyond, at
+    // 96 x 157184 x 2048 and five tiles, 70 us and more; the ring 69).  This form and
+    // the ring: 64 x 157184 x 2048 53 and 58 us, 128 x 157184 x 2048 90 and 97, 96 x
+    // 65536 x 4096 50 and 62, 128 x 65536 x 4096 61 and 76, 256 x 16384 x 4096 43 and 45.
+    if (dw && K % 256 == 0 && TT >= 4 && nt > 1 && TT * nt <= 24) {
+        auto pair = [&](auto tt, auto n) {
+            constexpr int T = decltype(tt)::value, M = decltype(n)::value;
+            const int groups = (tiles + kWaves * M - 1) / (kWaves * M);
+            void (*kernel)(MxArgs, PackView, int) = mx4_pair_kernel<T, M>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * ((rows16 + T - 1) / T))),
+                               dim3(kMxThreads), 0, stream, a, pv, groups);
+        };
+        auto pick = [&](auto tt) {
+            constexpr int T = decltype(tt)::value;
+            if (nt == 2) pair(tt, FB_C(2));
+            else if (nt == 3) pair(tt, FB_C(3));
+            else if constexpr (T <= 6) {
+                if (nt == 4) pair(tt, FB_C(4));
+                else if constexpr (T <= 4) pair(tt, FB_C(5));
+            }
+        };
+        if (TT == 4) pick(FB_C(4));
+        else if (TT == 6) pick(FB_C(6));
+        else pick(FB_C(8));
+        return hipGetLastError();
     }
     auto pick = [&](auto tt) {
         if (nt == 1) launch(tt, FB_C(1), FB_C(1));

@@ -180,11 +180,22 @@ def test_many_rows(rows, N, K):
     check_device(bt, *case, long_call(bt, *case, out), out)
 
 
+@pytest.mark.parametrize("rows", [40, 60, 90, 128, 150])
+@pytest.mark.parametrize("N,K", [(33001, 256), (65604, 1280), (70000, 512), (100004, 768),
+                                 (100016, 288), (140000, 512)])
+def test_long_outputs_many_rows(rows, N, K):
+    bt = Batch(w=[1], o=[3], bl=rows, W_max=1).cuda()
+    case = long_inputs(bt, N, K, seed=rows + K)
+    out = "bf16" if rows % 16 else "f32"
+    check_device(bt, *case, long_call(bt, *case, out), out)
+
+
+@pytest.mark.parametrize("bl", [3, 7, 16])
 @pytest.mark.parametrize("N", [9000, 65557])
 @pytest.mark.parametrize("K", [2016, 4096])
-def test_long_outputs_padded(N, K):
+def test_long_outputs_padded(N, K, bl):
     """Dead rows between live ones, their contents NaN; an infinite row; a NaN scale."""
-    bt = Batch(w=[1, 3, 2], o=[12, 7, 33], bl=3, W_max=3, layout="padded", inactive=(1,)).cuda()
+    bt = Batch(w=[1, 3, 2], o=[12, 7, 33], bl=bl, W_max=3, layout="padded", inactive=(1,)).cuda()
     codes, scales, x = long_inputs(bt, N, K, seed=4)
     y = long_call(bt, codes, scales, x, "f32")
     check_device(bt, codes, scales, x, y, "f32")
@@ -219,3 +230,22 @@ def test_long_output_nothing_live():
     bt = Batch(**BATCHES["nothing"]).cuda()
     case = long_inputs(bt, 65552, 1536)
     assert torch.all(long_call(bt, *case, "f32") == 5)
+
+
+def test_offsets_past_32_bits():
+    """Codes of 4.6 GB and outputs of 2.2e9 elements: sampled columns and rows."""
+    pick = np.r_[0:30, 600000:600030]
+    for rows, N, K in ((1, 1100003, 8352), (1, 2250000, 4096), (2200, 1000003, 512)):
+        bt = Batch(w=[1], o=[3], bl=rows, W_max=1).cuda()
+        codes, scales, x = long_inputs(bt, N, K, seed=K)
+        y = long_call(bt, codes, scales, x, "bf16")
+        cols = torch.from_numpy(np.r_[pick, N - 30:N]).cuda()
+        check_device(bt, codes[cols], scales[cols], x, y[:, cols], "bf16")
+        del codes, scales, x, y
+
+
+def test_widest_k():
+    for rows in (3, 96):
+        bt = Batch(w=[1], o=[3], bl=rows, W_max=1).cuda()
+        case = long_inputs(bt, 33, 65536, seed=rows)
+        check_device(bt, *case, long_call(bt, *case, "f32"), "f32")

@@ -134,3 +134,22 @@ def test_large_pack():
         fb.fb_residual_norm(*t.values(), h_out, n_out, bt.pack,
                             fb.make_norm_shape(D, "bf16", "request", EPS, A))
         check(bt, D, "bf16", "request", t, h_out, n_out)
+
+
+def test_offsets_past_32_bits():
+    """140800 rows of 16384: rows around element 2^31 and the last ones."""
+    D = 16384
+    bt = Batch(w=[4] * 1100, o=[32] * 1100, bl=32, W_max=4).cuda()
+    g = torch.Generator(device="cuda").manual_seed(0)
+    y, h = (torch.randn(bt.row_cap, D, generator=g, device="cuda", dtype=torch.bfloat16)
+            for _ in range(2))
+    w = torch.randn(D, generator=g, device="cuda").to(torch.bfloat16)
+    rows = np.r_[0, 2 ** 31 // D - 2:2 ** 31 // D + 2, bt.row_cap - 2:bt.row_cap]
+    assert np.isin(rows, bt.live).all()
+    h0 = f64(h[rows])
+    fb.fb_residual_norm(y, h, None, None, w, h, y, bt.pack,
+                        fb.make_norm_shape(D, "bf16", "none", EPS, 0.0))
+    assert np.array_equal(f64(h[rows]), h0)     # a = 0
+    n = h0 / np.sqrt((h0 * h0).mean(1, keepdims=True) + float(np.float32(EPS))) * f64(w)
+    tol = (160 * 2.0 ** -24 + HALF_STEP["bf16"]) * np.abs(n)
+    assert np.all(np.abs(f64(y[rows]) - n) <= tol)
