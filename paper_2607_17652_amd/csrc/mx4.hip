@@ -45,7 +45,7 @@ struct MxArgs {
     const uint8_t* codes;
     const uint8_t* scales;
     void* y;
-    int N, K, row_cap, bf16_out, vec_out;
+    int N, K, row_cap, bf16_out;
 };
 
 // Eight weights (one dword of codes) as the MFMA's A operand; the scale is a
@@ -71,6 +71,9 @@ __device__ inline void live_rows(const PackView& pv, int r0, int row_cap, uint64
     m1 = n > 64 ? __ballot(r + 64 < row_cap && pv.row_req[min(r + 64, row_cap - 1)] >= 0) : 0;
 }
 
+// Four neighbouring results; those past N fall away.  Rows of an N that is no multiple
+// of four start anywhere: the address unit takes them (900 x 12001 x 608 34.8 us with a
+// store for each result, 25.8 so).
 __device__ inline void store4(const MxArgs& a, int row, int n, const f32x4& v) {
     const size_t at = (size_t)row * a.N + n;
     if (a.bf16_out) {
@@ -78,21 +81,20 @@ __device__ inline void store4(const MxArgs& a, int row, int n, const f32x4& v) {
         uint16_t h[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (__bf16)v[i]);
-        if (a.vec_out && n < a.N) {
-            *reinterpret_cast<uint2*>(p) =
-                make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+        if (n + 4 <= a.N) {
+            __builtin_memcpy(p, h, 8);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 3; ++i)
                 if (n + i < a.N) p[i] = h[i];
         }
     } else {
         float* p = static_cast<float*>(a.y) + at;
-        if (a.vec_out && n < a.N) {
-            *reinterpret_cast<f32x4*>(p) = v;
+        if (n + 4 <= a.N) {
+            __builtin_memcpy(p, &v, 16);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 3; ++i)
                 if (n + i < a.N) p[i] = v[i];
         }
     }
@@ -679,8 +681,7 @@ hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scale
     PackView pv = pack_view(pack);
     const int cap = pack->row_cap;
     MxArgs a{static_cast<const uint16_t*>(x), static_cast<const uint8_t*>(codes),
-             static_cast<const uint8_t*>(scales), y, N, K, cap, y_dtype == FB_BF16 ? 1 : 0, 0};
-    a.vec_out = N % 4 == 0 && ((uintptr_t)y & (y_dtype == FB_BF16 ? 7 : 15)) == 0;
+             static_cast<const uint8_t*>(scales), y, N, K, cap, y_dtype == FB_BF16 ? 1 : 0};
     const int tiles = (N + 15) / 16;
     const bool dw = K % 128 == 0 && ((uintptr_t)scales & 3) == 0;
     auto launch = [&](auto tt, auto nt, auto kw) {
