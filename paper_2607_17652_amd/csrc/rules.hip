@@ -555,11 +555,21 @@ __device__ inline uint32_t window_entries(const RowRules& rr, int first, int str
     return lane < 32 ? rr.spans[v0 / kSpan].x : rr.spans[last].y;
 }
 
+// (p, x_hat) of a row from all of it.
+__device__ inline void predict(const Top& t, float* conf, int32_t* argmax) {
+    const float resid = fmaf(t.m, kLog2e, -t.mL);
+    const bool none = t.m == -INFINITY;
+    *conf = none ? 0.f : 1.0f / (t.s * __builtin_amdgcn_exp2f(-resid));
+    *argmax = none ? -1 : t.idx;
+}
+
+// `conf` and `argmax`, if not NULL, are written here: nsplit is 1 then.
 template <typename T>
 __global__ void __launch_bounds__(kVocabThreads, 8)
 vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
                    fb_logit_rules rules, RuleView rv, int mask_words,
-                   float4* __restrict__ part) {
+                   float4* __restrict__ part, float* __restrict__ conf,
+                   int32_t* __restrict__ argmax) {
     using W = Window<T>;
     __shared__ __attribute__((aligned(16))) typename W::Stage stages[kVocabThreads / 64];
     __shared__ Top wtop[kVocabThreads / 64];
@@ -572,7 +582,10 @@ vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const RowRules rr = row_rules(rules, rv, pv, row, req, mask_words);
     if (rr.none) {
-        if (tid == 0) part[(size_t)row * nsplit + k] = top_pack(top_empty());
+        if (tid == 0) {
+            part[(size_t)row * nsplit + k] = top_pack(top_empty());
+            if (conf) predict(top_empty(), conf + row, argmax + row);
+        }
         return;
     }
     const T* rp = logits + (size_t)row * V;
@@ -645,7 +658,10 @@ vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
             o.idx = __shfl_xor(t.idx, off, 64);
             t = top_merge(t, o);
         }
-        if (lane == 0) part[(size_t)row * nsplit + k] = top_pack(t);
+        if (lane == 0) {
+            part[(size_t)row * nsplit + k] = top_pack(t);
+            if (conf) predict(t, conf + row, argmax + row);
+        }
     };
     // whether some wave met a maximum, and whether anything is allowed
     if (lane == 0) s_met[wave] = (t.m > kLowest ? 1 : 0) | (any ? 2 : 0);
@@ -685,21 +701,22 @@ vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
     write();
 }
 
-// (p, x_hat) of every live row from its partials, as the update merges them.
+// (p, x_hat) of every live row from its partials, two or more, as the update merges
+// them.  (Rows of one partial are predicted by the pass itself.)
 constexpr int kPredictThreads = 256;
 
 __global__ void __launch_bounds__(kPredictThreads)
 predict_kernel(const float4* __restrict__ part, int nsplit, PackView pv, int row_cap,
                float* __restrict__ conf, int32_t* __restrict__ argmax) {
     const int row = blockIdx.x * kPredictThreads + threadIdx.x;
-    if (row >= row_cap || pv.row_req[row] < 0) return;
-    Top t = top_unpack(part[(size_t)row * nsplit]);
-    for (int k = 1; k < nsplit; ++k)
+    if (row >= row_cap) return;
+    // loaded together with the row's request
+    const float4 first = part[(size_t)row * nsplit], second = part[(size_t)row * nsplit + 1];
+    if (pv.row_req[row] < 0) return;
+    Top t = top_merge(top_unpack(first), top_unpack(second));
+    for (int k = 2; k < nsplit; ++k)
         t = top_merge(t, top_unpack(part[(size_t)row * nsplit + k]));
-    const float resid = fmaf(t.m, kLog2e, -t.mL);
-    const bool none = t.m == -INFINITY;
-    conf[row] = none ? 0.f : 1.0f / (t.s * __builtin_amdgcn_exp2f(-resid));
-    argmax[row] = none ? -1 : t.idx;
+    predict(t, conf + row, argmax + row);
 }
 
 template <typename T>
@@ -813,17 +830,20 @@ hipError_t launch_vocab_rules(const void* logits, int V, int dtype, const fb_pac
     PackView pv = pack_view(pack);
     const RuleView rv = rule_view(rz, const_cast<void*>(rules_ws));
     float4* part = static_cast<float4*>(upd_ws);
+    // one partial a row (V up to 16384): the pass predicts, a launch less
+    const bool one = uz.nsplit == 1;
     auto go = [&](auto zero) {
         using T = decltype(zero);
         hipLaunchKernelGGL(vocab_rules_kernel<T>,
                            dim3((unsigned)pack->row_cap * (unsigned)uz.nsplit),
                            dim3(kVocabThreads), 0, stream, static_cast<const T*>(logits), V,
-                           uz.nsplit, pv, *rules, rv, (V + 31) / 32, part);
+                           uz.nsplit, pv, *rules, rv, (V + 31) / 32, part,
+                           one ? conf : nullptr, one ? argmax : nullptr);
     };
     if (dtype == FB_BF16) go(uint16_t());
     else go(float());
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !conf) return e;
+    if (e != hipSuccess || !conf || one) return e;
     hipLaunchKernelGGL(predict_kernel,
                        dim3((pack->row_cap + kPredictThreads - 1) / kPredictThreads),
                        dim3(kPredictThreads), 0, stream, part, uz.nsplit, pv, pack->row_cap,
