@@ -622,7 +622,7 @@ struct Ring {
 };
 
 __device__ inline void dma16(const void* src, uint32_t lds_wave_base) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+    asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, off"
                  :: "s"(lds_wave_base), "v"(src) : "memory");
 }
 
@@ -835,7 +835,7 @@ attn_bf16_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k_
                 const bool isk = (RG_::kKCh % kAttnThreads == 0) ? (j * kAttnThreads < RG_::kKCh)
                                                                  : ld_isk[j];
                 const unsigned char* base = isk ? kbase : vbase;
-                asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+                asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, %2"
                              :: "s"(m0), "v"(ch_off[j]), "s"(base) : "memory");
             }
         } else {
@@ -853,7 +853,7 @@ attn_bf16_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k_
                 const unsigned char* src = (isk ? kb0 : vb0) + ch_off[j] +
                                            (size_t)(uint32_t)page * (size_t)page_bytes;
                 const uint32_t m0 = m0_base[j] + STAGE * RG_::kStageBytes;
-                asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+                asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, off"
                              :: "s"(m0), "v"(src) : "memory");
             }
         }
@@ -1485,7 +1485,7 @@ struct F32Tile {
 };
 
 __device__ inline void dma4(const void* src, uint32_t lds_wave_base) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+    asm volatile(FB_SET_M0 "global_load_lds_dword %1, off"
                  :: "s"(lds_wave_base), "v"(src) : "memory");
 }
 

@@ -52,6 +52,12 @@ __device__ inline void record_error(int32_t* hdr, int req, int code) {
     atomicMin(&hdr[kHdrStatus], req * 16 + code);
 }
 
+// Opens an asm string that loads straight into LDS: its first operand, the LDS
+// address, goes to M0.  A scalar write of M0 and a load to LDS that reads it need one
+// wait state between them; the compiler puts it in by itself, but not inside a
+// string.  (M0 is reserved: the compiler keeps nothing in it across statements.)
+#define FB_SET_M0 "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+
 // ---- launchers (each returns the launch status) ---------------------------
 hipError_t launch_pack(const fb_req_state* st, const int32_t* tokens, int n_max,
                        int T_max, const fb_pack* pack, hipStream_t stream);

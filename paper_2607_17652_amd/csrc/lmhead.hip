@@ -191,12 +191,12 @@ lm_few_rows(const uint16_t* __restrict__ H, const uint16_t* __restrict__ W, int 
         if (ld_live) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)   // read once: nontemporal
-                asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, %2 nt"
                              :: "s"(m0_w + so + j * 1024), "v"(w_off[j]), "s"(wb) : "memory");
         }
 #pragma unroll
         for (int j = 0; j < NH; ++j)
-            asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+            asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, %2"
                          :: "s"(m0_h + so + j * 1024), "v"(h_off[j]), "s"(hb) : "memory");
         ld_slot = ld_slot == kFewStages - 1 ? 0 : ld_slot + 1;
         if (++ld_ks == KS) {
@@ -431,11 +431,11 @@ lmhead_kernel(const uint16_t* __restrict__ H, const uint16_t* __restrict__ W, in
         const uint32_t so = stage * kStageBytes;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+            asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, %2"
                          :: "s"(m0_w[j] + so), "v"(w_off[j]), "s"(wb) : "memory");
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+            asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, %2"
                          :: "s"(m0_h[j] + so), "v"(h_off[j]), "s"(hb) : "memory");
     };
 

@@ -103,19 +103,19 @@ __device__ inline void store4(const MxArgs& a, int row, int n, const f32x4& v) {
 // Direct global->LDS loads; lane l's 16 bytes land at lds + 16 l (its byte,
 // widened, at lds + 4 l).
 __device__ inline void dma16(uint32_t lds, uint32_t off, const void* base) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+    asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, %2"
                  :: "s"(lds), "v"(off), "s"(base) : "memory");
 }
 __device__ inline void dma16(uint32_t lds, const void* p) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+    asm volatile(FB_SET_M0 "global_load_lds_dwordx4 %1, off"
                  :: "s"(lds), "v"(p) : "memory");
 }
 __device__ inline void dma4(uint32_t lds, uint32_t off, const void* base) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2"
+    asm volatile(FB_SET_M0 "global_load_lds_dword %1, %2"
                  :: "s"(lds), "v"(off), "s"(base) : "memory");
 }
 __device__ inline void dma1(uint32_t lds, uint32_t off, const void* base) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_ubyte %1, %2"
+    asm volatile(FB_SET_M0 "global_load_lds_ubyte %1, %2"
                  :: "s"(lds), "v"(off), "s"(base) : "memory");
 }
 
