@@ -67,6 +67,14 @@ __device__ inline void workgroup_sync() {
     __syncthreads();
 }
 
+// What the wave's lanes wrote to LDS before this is what each of them reads after it.
+// The hardware keeps a wave's LDS operations in order; the compiler may not, since
+// for it another lane's store is another thread's.  No instruction comes of it.
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Calls f(i, token - v0) for the tokens of [0, n) that lie in [v0, v0 + nv), the
 // loads of eight rounds in flight together: one token a load up to 8192 of them
 // (one round trip, every lane at work), four neighbours beyond.
@@ -620,6 +628,7 @@ vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
             // the touched tokens are taken out of the staged window, adjusted and
             // folded one a lane; the rest folds below
             w.stage(stage);
+            wave_sync();
             for (int e = e0; e < e1; e += 64) {
                 const uint2 a = adj;
                 if (e + 64 + lane < e1) adj = rr.adj[e + 64 + lane];
@@ -632,6 +641,7 @@ vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
                 }
                 wt.fold<1, 1>(f, v);
             }
+            wave_sync();
             w.fetch(stage);
         }
 #pragma unroll
@@ -760,6 +770,7 @@ logits_rules_kernel(const T* logits, T* out, int V, int nsplit, PackView pv,
         if (some && rr.mask) w.mask(allowed);
         if (e1 > e0) {   // uniform
             w.stage(stage);
+            wave_sync();
             for (int e = e0; e < e1; e += 64) {
                 const uint2 a = adj;
                 if (e + 64 + lane < e1) adj = rr.adj[e + 64 + lane];
@@ -770,6 +781,7 @@ logits_rules_kernel(const T* logits, T* out, int V, int nsplit, PackView pv,
                     else z = f;
                 }
             }
+            wave_sync();
             w.fetch(stage);
         }
 #pragma unroll
