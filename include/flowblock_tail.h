@@ -52,6 +52,8 @@ typedef struct fb_norm_shape {
  *   n    = h' / sqrt(mean(h'^2) + eps) * w_pre -> n_out
  * with g the gate (its layout in sh) and a = res_scale.  Everything between
  * the inputs and the two outputs is float32; n is formed from the unrounded h'.
+ * The norms hold for every finite y and h', also where the squares or their mean
+ * pass float32's range.
  *   y       [row_cap][D], the block's output; NULL for a plain norm of h (then
  *           gate, w_post and h_out are NULL too)
  *   h       [row_cap][D], the residual stream

@@ -96,16 +96,34 @@ __device__ inline float row_sum(float v, float* lds) {
     return v;
 }
 
+// 1 / sqrt(mean(x^2) + eps) of a row from the lane's sum of squares; all lanes of the row
+// get the same.  Where the squares or their sum leave the float range (entries of 1e18
+// at D = 1024, say), small_squares() sums them again with the entries taken 2^72 times
+// smaller: the largest float squares to 2^112 then, 16384 of them make 2^126, and what
+// has to be there for the first sum to overflow is far from underflow.  (Past a root
+// mean square of 2^126 the result is subnormal, two bits fewer at most.)
+constexpr float kSmall = 0x1p-72f;
+
+template <int WR, typename F>
+__device__ inline float inverse_rms(float squares, F&& small_squares, const NormArgs& a,
+                                    float (*lds)[WR]) {
+    const float q = row_sum<WR>(squares, lds[0]);
+    if (q < INFINITY) return 1.f / sqrtf(q / (float)a.D + a.eps);
+    const float d = row_sum<WR>(small_squares(), lds[1]);   // infinities and NaN stay
+    return kSmall / sqrtf(d / (float)a.D + a.eps * kSmall * kSmall);
+}
+
 // RW rows a workgroup, each of WR waves (RW is 1 where WR is more than 1).
-// EARLY: the weights, the gate and, before it is known that the row is live,
-// the row itself are loaded together, for calls of few rows, whose time is the
-// chain of loads that wait for one another.
+// EARLY: before it is known that the row is live it is loaded, and with it (WEIGHTS)
+// the weights and the gate, for calls of few rows, whose time is the chain of loads that
+// wait for one another.  Rows of more than two chunks a lane leave no registers for the
+// weights (96 rows of 16384 in fp32: 9.9 us, 15.1 with 80 registers spilled).
 template <typename T, int WR, int RW, int NC, bool EARLY>
 __global__ void __launch_bounds__(64 * WR * RW)
 residual_norm_kernel(NormArgs a, PackView pv, int row_cap) {
     using V = Chunk<T>;
     constexpr int N = V::N;
-    __shared__ float red[2][WR > 1 ? WR : 1];
+    __shared__ float red[4][WR];
     const int row = blockIdx.x * RW + (RW > 1 ? threadIdx.x >> 6 : 0);
     if (RW > 1 && row >= row_cap) return;
     const int req = pv.row_req[row];
@@ -116,6 +134,10 @@ residual_norm_kernel(NormArgs a, PackView pv, int row_cap) {
     const T* y = static_cast<const T*>(a.y);
     if (y) y += at;
 
+    // A row's partial chunk is loaded after all whole ones where its loads are packed
+    // and so waited for (bf16): 21216 rows of 4096 130 us, 133 in between; in between
+    // in fp32: 4704 rows of 2011 40.1 us, 41.0 last.
+    constexpr bool TAIL_LAST = sizeof(T) == 2;
     u32x4 hv[NC], yv[NC];
     int left[NC];      // elements of the lane's chunk that lie in the row
     int pos[NC];
@@ -127,10 +149,18 @@ residual_norm_kernel(NormArgs a, PackView pv, int row_cap) {
         if (left[c] >= N) {
             hv[c] = V::load(h + pos[c]);
             if (y) yv[c] = V::load(y + pos[c]);
-        } else if (left[c] > 0) {
+        } else if (!TAIL_LAST && left[c] > 0) {
             hv[c] = V::load(h + pos[c], left[c]);
             if (y) yv[c] = V::load(y + pos[c], left[c]);
         }
+    }
+    if constexpr (TAIL_LAST) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            if (left[c] > 0 && left[c] < N) {
+                hv[c] = V::load(h + pos[c], left[c]);
+                if (y) yv[c] = V::load(y + pos[c], left[c]);
+            }
     }
     auto load = [&](const T* w, int c) {
         if (left[c] >= N) return V::load(w + pos[c]);
@@ -141,8 +171,13 @@ residual_norm_kernel(NormArgs a, PackView pv, int row_cap) {
     const T* g = static_cast<const T*>(a.gate);
     if (a.gate_kind == FB_GATE_REQUEST) g += (size_t)max(req, 0) * a.D;
     if (a.gate_kind == FB_GATE_ROW) g += at;
-    u32x4 early[3][EARLY ? NC : 1];
-    if constexpr (EARLY) {
+    constexpr bool WEIGHTS = EARLY && NC <= 2;
+    u32x4 early[3][WEIGHTS ? NC : 1];
+    if (EARLY && !WEIGHTS) {
+        asm volatile("" ::: "memory");   // the loads above stay above
+        if (req < 0) return;
+    }
+    if constexpr (WEIGHTS) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             if (w_post) early[0][c] = load(w_post, c);
@@ -156,7 +191,7 @@ residual_norm_kernel(NormArgs a, PackView pv, int row_cap) {
         asm volatile("" ::: "memory");
     }
     auto weight = [&](const T* w, int k, int c, float (&f)[N]) {
-        V::unpack(EARLY ? early[k][EARLY ? c : 0] : load(w, c), f);
+        V::unpack(WEIGHTS ? early[k][WEIGHTS ? c : 0] : load(w, c), f);
     };
 
     float hp[NC][N];
@@ -172,7 +207,19 @@ residual_norm_kernel(NormArgs a, PackView pv, int row_cap) {
 #pragma unroll
                 for (int j = 0; j < N; ++j) q = fmaf(f[j], f[j], q);
             }
-            r = 1.f / sqrtf(row_sum<WR>(q, red[0]) / (float)a.D + a.eps);
+            r = inverse_rms<WR>(q, [&] {
+                float d = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    float f[N];
+                    u32x4 v = yv[c];
+                    asm("" : "+v"(v));   // unpacked anew: else it is at the loads, which then wait
+                    V::unpack(v, f);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) d = fmaf(kSmall * f[j], kSmall * f[j], d);
+                }
+                return d;
+            }, a, red);
         }
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -205,7 +252,14 @@ residual_norm_kernel(NormArgs a, PackView pv, int row_cap) {
         }
     }
     if (!a.n_out) return;
-    const float r = 1.f / sqrtf(row_sum<WR>(s, red[1]) / (float)a.D + a.eps);
+    const float r = inverse_rms<WR>(s, [&] {
+        float d = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < N; ++j) d = fmaf(kSmall * hp[c][j], kSmall * hp[c][j], d);
+        return d;
+    }, a, red + 2);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         if (left[c] <= 0) continue;
