@@ -552,15 +552,25 @@ struct Window {
 };
 
 // The entries of the wave's windows: lane i has the first of its i-th window's,
-// lane 32 + i one past the last (at most 32 windows: V is at most 2^19).
+// lane 32 + i one past the last.  A row of 2^19 float32 logits is 64 pieces, so its
+// workgroups have to be two at least; update_sizes makes them two, and the launchers
+// refuse what does not fit.
+constexpr int kMaxWindows = 32;
+
+template <typename T>
+inline bool walk_fits(int V, int nsplit) {
+    const int round = nsplit * Window<T>::kPiece;
+    return (V + round - 1) / round <= kMaxWindows;
+}
+
 template <typename T>
 __device__ inline uint32_t window_entries(const RowRules& rr, int first, int stride, int V) {
     if (!rr.bits) return 0;
     const int lane = threadIdx.x & 63;
-    const int v0 = first + (lane & 31) * stride;
+    const int v0 = first + (lane & (kMaxWindows - 1)) * stride;
     if (v0 >= V) return 0;
     const int last = min((v0 + Window<T>::kTokens) / kSpan, (V + kSpan - 1) / kSpan) - 1;
-    return lane < 32 ? rr.spans[v0 / kSpan].x : rr.spans[last].y;
+    return lane < kMaxWindows ? rr.spans[v0 / kSpan].x : rr.spans[last].y;
 }
 
 // (p, x_hat) of a row from all of it.
@@ -618,7 +628,7 @@ vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
         }
         any = true;
         const int e0 = __builtin_amdgcn_readlane(entries, i);
-        const int e1 = __builtin_amdgcn_readlane(entries, 32 + i);
+        const int e1 = __builtin_amdgcn_readlane(entries, kMaxWindows + i);
         W w;
         w.load(rp, v0, V);
         uint2 adj = make_uint2(0, (uint32_t)v0);
@@ -693,7 +703,7 @@ vocab_rules_kernel(const T* __restrict__ logits, int V, int nsplit, PackView pv,
                 if ((rr.allowed(v & ~7) >> (v & 7) & 1) &&
                     !(rr.bits && rr.bits[v >> 3] >> (v & 7) & 1))
                     take(v, value(rp[v]));
-            const int e1 = __builtin_amdgcn_readlane(entries, 32 + i);
+            const int e1 = __builtin_amdgcn_readlane(entries, kMaxWindows + i);
             for (int e = __builtin_amdgcn_readlane(entries, i) + lane; e < e1; e += 64) {
                 const uint2 a = rr.adj[e];
                 const int v = (int)(a.y & ~kSeen);
@@ -761,7 +771,7 @@ logits_rules_kernel(const T* logits, T* out, int V, int nsplit, PackView pv,
             if (v0 + stride < V) next.load(rr.mask, v0 + stride, V);
         }
         const int e0 = __builtin_amdgcn_readlane(entries, i);
-        const int e1 = some ? __builtin_amdgcn_readlane(entries, 32 + i) : e0;
+        const int e1 = some ? __builtin_amdgcn_readlane(entries, kMaxWindows + i) : e0;
         W w;
         if (some) w.load(rp, v0, V);
         else w.fill();
@@ -846,15 +856,15 @@ hipError_t launch_vocab_rules(const void* logits, int V, int dtype, const fb_pac
     const bool one = uz.nsplit == 1;
     auto go = [&](auto zero) {
         using T = decltype(zero);
+        if (!walk_fits<T>(V, uz.nsplit)) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL(vocab_rules_kernel<T>,
                            dim3((unsigned)pack->row_cap * (unsigned)uz.nsplit),
                            dim3(kVocabThreads), 0, stream, static_cast<const T*>(logits), V,
                            uz.nsplit, pv, *rules, rv, (V + 31) / 32, part,
                            one ? conf : nullptr, one ? argmax : nullptr);
+        return hipGetLastError();
     };
-    if (dtype == FB_BF16) go(uint16_t());
-    else go(float());
-    hipError_t e = hipGetLastError();
+    const hipError_t e = dtype == FB_BF16 ? go(uint16_t()) : go(float());
     if (e != hipSuccess || !conf || one) return e;
     hipLaunchKernelGGL(predict_kernel,
                        dim3((pack->row_cap + kPredictThreads - 1) / kPredictThreads),
@@ -870,15 +880,15 @@ hipError_t launch_logits_rules(const void* logits, void* out, int V, int dtype,
     const RuleView rv = rule_view(rz, const_cast<void*>(rules_ws));
     auto go = [&](auto zero) {
         using T = decltype(zero);
+        if (!walk_fits<T>(V, uz.nsplit)) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL(logits_rules_kernel<T>,
                            dim3((unsigned)pack->row_cap * (unsigned)uz.nsplit),
                            dim3(kVocabThreads), 0, stream, static_cast<const T*>(logits),
                            static_cast<T*>(out), V, uz.nsplit, pack_view(pack), *rules, rv,
                            (V + 31) / 32);
+        return hipGetLastError();
     };
-    if (dtype == FB_BF16) go(uint16_t());
-    else go(float());
-    return hipGetLastError();
+    return dtype == FB_BF16 ? go(uint16_t()) : go(float());
 }
 
 }  // namespace fb
