@@ -28,6 +28,7 @@ FB_DERR_RULE = 4
 
 FB_F32 = 0
 FB_BF16 = 1
+FB_I32 = -1       # for _type alone: no call takes it
 FB_RAGGED = 0
 FB_PADDED = 1
 FB_EDIT_MASKED = 1
@@ -119,6 +120,7 @@ class fb_logit_rules(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("params", "bias_start", "bias_id", "bias_val", "masks", "row_mask")] + \
         [("n_bias", ctypes.c_int32), ("n_masks", ctypes.c_int32)]
+    tensors = (None,) * 6       # make_rules: what the pointers belong to
 
 
 # numpy views of the device records
@@ -212,7 +214,7 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-_torch = None
+_raw_stream = _device = None     # torch's calls, once CUDA is up
 
 
 def _stream(stream):
@@ -221,23 +223,41 @@ def _stream(stream):
     about a third of a call."""
     if stream is not None:
         return stream.cuda_stream
-    global _torch
-    if _torch is None:
-        import torch
-        _torch = torch
-    c = _torch._C
-    if _torch.cuda.is_initialized() and hasattr(c, "_cuda_getCurrentRawStream"):
-        return c._cuda_getCurrentRawStream(c._cuda_getDevice())
-    return _torch.cuda.current_stream().cuda_stream
+    global _raw_stream, _device
+    if _raw_stream is not None:
+        return _raw_stream(_device())
+    import torch
+    c = torch._C
+    if torch.cuda.is_initialized() and hasattr(c, "_cuda_getCurrentRawStream"):
+        _raw_stream, _device = c._cuda_getCurrentRawStream, c._cuda_getDevice
+    return torch.cuda.current_stream().cuda_stream
+
+
+_types, _codes = {}, {}      # dtype code -> torch type and back; the library's int32
+
+
+def _load_types():
+    import torch
+    _types.update({FB_BF16: torch.bfloat16, FB_F32: torch.float32, FB_I32: torch.int32})
+    _codes.update({torch.bfloat16: FB_BF16, torch.float32: FB_F32})
+
+
+def _type(code):
+    if not _types:
+        _load_types()
+    t = _types.get(code)
+    if t is None:
+        raise FlowBlockError(FB_E_UNSUPPORTED, f"dtype {code}")
+    return t
 
 
 def _dtype_code(t):
-    import torch
-    if t.dtype == torch.bfloat16:
-        return FB_BF16
-    if t.dtype == torch.float32:
-        return FB_F32
-    raise FlowBlockError(FB_E_UNSUPPORTED, f"dtype {t.dtype}")
+    if not _codes:
+        _load_types()
+    code = _codes.get(t.dtype)
+    if code is None:
+        raise FlowBlockError(FB_E_UNSUPPORTED, f"dtype {t.dtype}")
+    return code
 
 
 # ------------------------------------------------------------------ library
@@ -266,10 +286,7 @@ class Pack:
     def __init__(self, handle, buf):
         self.handle = handle
         self.buf = buf
-
-    @property
-    def row_cap(self):
-        return self.handle.row_cap
+        self.B, self.row_cap = handle.B, handle.row_cap
 
     @property
     def tile_cap(self):
@@ -447,6 +464,49 @@ def stats_to_numpy(stats_tensor, B):
 
 
 # ------------------------------------------------------- the model's tail
+# These calls take many tensors that have to agree.  What the library cannot see of
+# them is checked here: the element type, that they are dense and on the GPU, and that
+# they hold all that the call reads or writes.  (Structs go to the library as they are:
+# ctypes passes their address in 0.27 us less than a reference made here.)
+def _dense(t, dtype, n, name):
+    """The pointer of t (None: NULL), which holds n elements of `dtype` or more."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.numel() >= n and t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
+    return _refuse(t, dtype, n, name)
+
+
+def _refuse(t, dtype, n, name):
+    if dtype is not None and t.dtype is not dtype:
+        why = f"holds {t.dtype}, not {dtype}"
+    elif t.numel() < n:
+        why = f"has {t.numel()} elements, needs {n}"
+    elif not t.is_contiguous():
+        why = "is not contiguous"
+    else:
+        why = "is not on the GPU"
+    raise FlowBlockError(FB_E_INVAL, f"{name} {why}")
+
+
+def _octets(t, n, name):
+    """The pointer of t, n bytes in elements of one byte, whatever they are called."""
+    if t.element_size() != 1:
+        raise FlowBlockError(FB_E_INVAL, f"{name} holds {t.dtype}, not bytes")
+    if t.numel() != n:
+        raise FlowBlockError(FB_E_INVAL, f"{name} has {t.numel()} bytes, not {n}")
+    if t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
+    return _refuse(t, None, n, name)
+
+
+def _space(ws, name):
+    """The pointer of a workspace; the library compares its size."""
+    if ws.is_contiguous() and ws.is_cuda:
+        return ws.data_ptr()
+    return _refuse(ws, None, 0, name)
+
+
 def make_norm_shape(D, dtype, gate="none", eps=1e-6, res_scale=1.0):
     if not isinstance(dtype, int):
         dtype = FB_BF16 if str(dtype) in ("bf16", "torch.bfloat16") else FB_F32
@@ -456,17 +516,26 @@ def make_norm_shape(D, dtype, gate="none", eps=1e-6, res_scale=1.0):
 
 def fb_residual_norm(y, h, gate, w_post, w_pre, h_out, n_out, pack, shape, stream=None):
     """u = rms(y) w_post, h_out = h + a g u, n_out = rms(h_out) w_pre on the live
-    rows; any of y, gate, w_post, w_pre, h_out, n_out may be None as the header says."""
-    _check(lib().fb_residual_norm(_ptr(y), _ptr(h), _ptr(gate), _ptr(w_post), _ptr(w_pre),
-                                  _ptr(h_out), _ptr(n_out), pack.ref(), ctypes.byref(shape),
-                                  _stream(stream)))
+    rows; any of y, gate, w_post, w_pre, h_out, n_out may be None as the header says.
+    All are of the shape's type."""
+    t, D = _type(shape.dtype), shape.D
+    n = pack.row_cap * D
+    if gate is not None:
+        gate = _dense(gate, t, {1: D, 2: pack.B * D, 3: n}.get(shape.gate, 0), "gate")
+    _check(lib().fb_residual_norm(_dense(y, t, n, "y"), _dense(h, t, n, "h"), gate,
+                                  _dense(w_post, t, D, "w_post"), _dense(w_pre, t, D, "w_pre"),
+                                  _dense(h_out, t, n, "h_out"), _dense(n_out, t, n, "n_out"),
+                                  pack.handle, shape, _stream(stream)))
 
 
 def fb_mx4_linear(x, codes, scales, pack, y, stream=None):
     """x bf16 [row_cap, K]; codes uint8 [N, K/2] (E2M1, element 2i in the low half
     of byte i); scales uint8 [N, K/32] (E8M0); y [row_cap, N], bf16 or fp32."""
-    _check(lib().fb_mx4_linear(_ptr(x), _ptr(codes), _ptr(scales), codes.shape[0],
-                               x.shape[-1], pack.ref(), _ptr(y), _dtype_code(y),
+    N, K, rows = codes.shape[0], x.shape[-1], pack.row_cap
+    _check(lib().fb_mx4_linear(_dense(x, _type(FB_BF16), rows * K, "x"),
+                               _octets(codes, N * K // 2, "codes"),
+                               _octets(scales, N * K // 32, "scales"), N, K, pack.handle,
+                               _dense(y, y.dtype, rows * N, "y"), _dtype_code(y),
                                _stream(stream)))
 
 
@@ -475,38 +544,71 @@ def make_rules(params=None, bias_start=None, bias_id=None, bias_val=None, masks=
     """params fp32 [B, 4] (repetition, presence, frequency, 0); bias_start int32
     [B+1] with bias_id int32 and bias_val fp32; masks int32 [n_masks,
     ceil(V/32)] with row_mask int32 [row_cap].  Keeps its tensors alive."""
-    r = fb_logit_rules(_ptr(params), _ptr(bias_start), _ptr(bias_id), _ptr(bias_val),
-                       _ptr(masks), _ptr(row_mask), 0 if bias_id is None else bias_id.numel(),
-                       0 if masks is None else masks.shape[0])
+    import torch
+    n_bias = 0 if bias_id is None else bias_id.numel()
+    n_masks = 0 if masks is None else masks.numel() // max(1, masks.shape[-1])
+    word = torch.int32 if masks is None or masks.dtype is not torch.uint32 else torch.uint32
+    r = fb_logit_rules(_dense(params, torch.float32, 0, "params"),
+                       _dense(bias_start, torch.int32, 0, "bias_start"),
+                       _dense(bias_id, torch.int32, 0, "bias_id"),
+                       _dense(bias_val, torch.float32, n_bias, "bias_val"),
+                       _dense(masks, word, 0, "masks"),
+                       _dense(row_mask, torch.int32, 0, "row_mask"), n_bias, n_masks)
     r.tensors = (params, bias_start, bias_id, bias_val, masks, row_mask)
     return r
 
 
+def _rules(rules, pack, V=0):
+    """The rules, which fit the pack and, for the calls that read masks,
+    the vocabulary."""
+    params, start, _, _, masks, row_mask = rules.tensors
+    if params is not None and params.numel() < 4 * pack.B:
+        _refuse(params, None, 4 * pack.B, "params")
+    if start is not None and start.numel() <= pack.B:
+        _refuse(start, None, pack.B + 1, "bias_start")
+    if V and masks is not None:
+        if masks.shape[-1] != (V + 31) // 32:
+            raise FlowBlockError(FB_E_INVAL, f"masks have rows of {masks.shape[-1]} words, not "
+                                             f"the {(V + 31) // 32} of {V} tokens")
+        if row_mask is not None and row_mask.numel() < pack.row_cap:
+            _refuse(row_mask, None, pack.row_cap, "row_mask")
+    return rules
+
+
 def fb_rules_workspace_bytes(pack, V):
-    return int(lib().fb_rules_workspace_bytes(pack.ref(), V))
+    return int(lib().fb_rules_workspace_bytes(pack.handle, V))
 
 
 def fb_rules_build(rules, st, tokens, V, pack, ws, stream=None):
-    _check(lib().fb_rules_build(ctypes.byref(rules), _ptr(st), _ptr(tokens), tokens.shape[-1], V,
-                                pack.ref(), _ptr(ws), ws.numel() * ws.element_size(),
-                                _stream(stream)))
+    B, T_max = pack.B, tokens.shape[-1]
+    if st is not None and st.nbytes < 32 * B:
+        raise FlowBlockError(FB_E_INVAL, f"st has {st.nbytes} bytes, needs {32 * B}")
+    _check(lib().fb_rules_build(_rules(rules, pack), st if st is None else _space(st, "st"),
+                                _dense(tokens, _type(FB_I32), B * T_max, "tokens"), T_max, V,
+                                pack.handle, _space(ws, "ws"), ws.nbytes, _stream(stream)))
 
 
 def fb_vocab_reduce_rules(logits, pack, rules, rules_ws, upd_ws, conf=None, argmax=None,
                           stream=None):
     """The reduction under the rules lands in upd_ws for fb_denoise_apply, and, if
     given, in conf fp32 and argmax int32 [row_cap]."""
-    _check(lib().fb_vocab_reduce_rules(_ptr(logits), logits.shape[-1], _dtype_code(logits),
-                                       pack.ref(), ctypes.byref(rules), _ptr(rules_ws),
-                                       rules_ws.numel() * rules_ws.element_size(), _ptr(upd_ws),
-                                       upd_ws.numel() * upd_ws.element_size(), _ptr(conf),
-                                       _ptr(argmax), _stream(stream)))
+    V, rows = logits.shape[-1], pack.row_cap
+    _check(lib().fb_vocab_reduce_rules(_dense(logits, logits.dtype, rows * V, "logits"), V,
+                                       _dtype_code(logits), pack.handle,
+                                       _rules(rules, pack, V), _space(rules_ws, "rules_ws"),
+                                       rules_ws.nbytes, _space(upd_ws, "upd_ws"), upd_ws.nbytes,
+                                       _dense(conf, _type(FB_F32), rows, "conf"),
+                                       _dense(argmax, _type(FB_I32), rows, "argmax"),
+                                       _stream(stream)))
 
 
 def fb_logits_rules(logits, out, pack, rules, rules_ws, stream=None):
-    _check(lib().fb_logits_rules(_ptr(logits), _ptr(out), logits.shape[-1], _dtype_code(logits),
-                                 pack.ref(), ctypes.byref(rules), _ptr(rules_ws),
-                                 rules_ws.numel() * rules_ws.element_size(), _stream(stream)))
+    V, t = logits.shape[-1], logits.dtype
+    n = pack.row_cap * V
+    _check(lib().fb_logits_rules(_dense(logits, t, n, "logits"), _dense(out, t, n, "out"), V,
+                                 _dtype_code(logits), pack.handle, _rules(rules, pack, V),
+                                 _space(rules_ws, "rules_ws"), rules_ws.nbytes,
+                                 _stream(stream)))
 
 
 # ------------------------------------------------------ multi-step loop
