@@ -275,12 +275,15 @@ rules_build_kernel(fb_logit_rules rules, const fb_req_state* __restrict__ st,
 
 // z' of a touched token.  z / r is the correctly rounded quotient: z times the
 // rounded reciprocal, corrected once by its exact remainder (Markstein, "Computation
-// of elementary functions on the IBM RISC System/6000 processor", 1990).  Past the
-// type's range it is the infinity that the product is.
+// of elementary functions on the IBM RISC System/6000 processor", 1990).  The remainder
+// is exact while its last bit, 2^-47 of z, is a float: from z = 2^-80 on, where the
+// quotient is normal too.  Smaller logits, and quotients whose first step overflows, are
+// divided.
 __device__ inline float adjust(float z, const uint2& adj, const float2& rec) {
 #pragma clang fp contract(off)
     const float q = z * rec.y;
-    const float div = finite(q) ? fmaf(fmaf(-q, rec.x, z), rec.y, q) : q;
+    float div = fmaf(fmaf(-q, rec.x, z), rec.y, q);
+    if (z > 0.f && (z < 0x1p-80f || !finite(q))) div = z / rec.x;
     const float pen = z > 0.f ? div : z * rec.x;
     return (adj.y & kSeen ? pen : z) + __uint_as_float(adj.x);
 }
