@@ -23,6 +23,7 @@ import hashlib
 import json
 import os
 import platform
+import re
 import sys
 import time
 
@@ -104,10 +105,26 @@ def workload_work(wl, host):
     return n_live, flops, kv_bytes + qo_bytes
 
 
+CSRC = os.path.join(ROOT, "paper_2607_17652_amd", "csrc")
+
+
+def kernel_files(name, known=()):
+    """A kernel's source and the headers beside it that it includes, directly or not."""
+    files = list(known) + [name]
+    with open(os.path.join(CSRC, name)) as f:
+        for inc in re.findall(r'^#include "([^"]+)"', f.read(), re.M):
+            if inc not in files and os.path.exists(os.path.join(CSRC, inc)):
+                files = kernel_files(inc, files)
+    return files
+
+
 def src_sha(name):
-    path = os.path.join(ROOT, "paper_2607_17652_amd", "csrc", name)
-    with open(path, "rb") as f:
-        return hashlib.sha256(f.read()).hexdigest()[:16]
+    """Of everything that a kernel's code comes from: parts of it stand in headers."""
+    h = hashlib.sha256()
+    for part in kernel_files(name):
+        with open(os.path.join(CSRC, part), "rb") as f:
+            h.update(f.read())
+    return h.hexdigest()[:16]
 
 
 def measured_traffic(kernel, workload, src_file):
