@@ -341,8 +341,9 @@ size_t fb_update_workspace_bytes(const fb_pack* pack, int V);
  *  over them passes theta_spawn.  Active requests whose (L, R, n) differ are
  *  recorded as FB_DERR_STATE and no request retires or admits in that call.
  *   logits  [row_cap][V], dtype FB_BF16 or FB_F32; rows not live are not read;
- *           a live row holds no NaN or +inf and at least one finite value
- *           (-inf entries are allowed and weigh exp(-inf) = 0)
+ *           a live row holds no NaN or +inf and at least one finite value,
+ *           none above 2^30 (-inf entries are allowed and weigh exp(-inf) = 0;
+ *           so are values down to the type's lowest)
  *   tokens  int32[B][T_max], updated in place
  *   conf, argmax  [row_cap]; only live rows are written
  *   st      fb_req_state[B], updated in place

@@ -49,7 +49,7 @@ vocab_pass_kernel(const T* __restrict__ logits, int V, int nsplit,
     if (a > V) a = V;
     const int e = a + ((V - a) / N) * N;
 
-    Top t = top_empty();
+    Top t = top_low();
     if (k == 0 && tid < a) {
         float f[1] = {VT::scalar(rp + tid)};
         top_fold<1>(t, f, tid);
@@ -92,11 +92,32 @@ vocab_pass_kernel(const T* __restrict__ logits, int V, int nsplit,
     __shared__ Top wtop[kVocabThreads / 64];
     if ((tid & 63) == 0) wtop[tid >> 6] = t;
     __syncthreads();
-    if (tid == 0) {
-        Top r = wtop[0];
-        for (int w = 1; w < kVocabThreads / 64; ++w) r = top_merge(r, wtop[w]);
-        part[(size_t)row * nsplit + k] = make_float4(r.m, r.s, __int_as_float(r.idx), r.mL);
+    if (tid >= 64) return;
+    Top r = wtop[0];
+    for (int w = 1; w < kVocabThreads / 64; ++w) r = top_merge(r, wtop[w]);
+    if (r.m == kLow) {   // uniform, and rare: nothing above kLow in the share
+        r = Top{-INFINITY, kLowRef, 0.f, 0x7fffffff};
+        auto count = [&](float m, float n, int v) {
+            if (m > r.m) r.s = 0.f, r.idx = 0x7fffffff, r.m = m;
+            if (m == r.m && m > -INFINITY) r.s += n, r.idx = min(r.idx, v);
+        };
+        auto walk = [&](int lo, int hi) {
+            for (int v = lo + tid; v < hi; v += 64) count(VT::scalar(rp + v), 1.f, v);
+        };
+        if (k == 0) {
+            walk(0, a);
+            walk(e, V);
+        }
+        for (int base = a + k * piece; base < e; base += nsplit * piece)
+            walk(base, min(base + piece, e));
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            const float m = __shfl_xor(r.m, off, 64), n = __shfl_xor(r.s, off, 64);
+            count(m, n, __shfl_xor(r.idx, off, 64));
+        }
+        if (r.m == -INFINITY) r = top_empty();
     }
+    if (tid == 0) part[(size_t)row * nsplit + k] = top_pack(r);
 }
 
 struct UpdParams {
@@ -168,17 +189,15 @@ request_kernel(const float4* __restrict__ part, int nsplit, PackView pv,
 #pragma unroll
         for (int k = 1; k < kPre; ++k)
             if (k < nsplit)
-                t = top_merge(t, Top{pre[k][0], pre[k][3], pre[k][1], __float_as_int(pre[k][2])});
+                t = top_merge_shares(t, Top{pre[k][0], pre[k][3], pre[k][1], __float_as_int(pre[k][2])});
         for (int k = kPre; k < nsplit; ++k) {
             const float4 pk = pr[k];
-            t = top_merge(t, Top{pk.x, pk.w, pk.y, __float_as_int(pk.z)});
+            t = top_merge_shares(t, Top{pk.x, pk.w, pk.y, __float_as_int(pk.z)});
         }
-        // s is relative to round(m*log2e); undo that rounding exactly.
-        const float resid = fmaf(t.m, kLog2e, -t.mL);
         // A row of nothing but -inf (rules that leave nothing) predicts
         // nothing: confidence 0 and, below, the one id that is never written.
         const bool none = t.m == -INFINITY;
-        const float conf = none ? 0.0f : 1.0f / (t.s * __builtin_amdgcn_exp2f(-resid));
+        const float conf = top_confidence(t);
         const int xhat = none ? prm.mask_id : t.idx;
         const bool masked = x == prm.mask_id;
         const bool prompt = pos < s.prompt_len;

@@ -578,10 +578,8 @@ __device__ inline uint32_t window_entries(const RowRules& rr, int first, int str
 
 // (p, x_hat) of a row from all of it.
 __device__ inline void predict(const Top& t, float* conf, int32_t* argmax) {
-    const float resid = fmaf(t.m, kLog2e, -t.mL);
-    const bool none = t.m == -INFINITY;
-    *conf = none ? 0.f : 1.0f / (t.s * __builtin_amdgcn_exp2f(-resid));
-    *argmax = none ? -1 : t.idx;
+    *conf = top_confidence(t);
+    *argmax = t.m == -INFINITY ? -1 : t.idx;
 }
 
 // `conf` and `argmax`, if not NULL, are written here: nsplit is 1 then.

@@ -24,6 +24,9 @@ __device__ inline float max_of(const float (&f)[N]) {
     }
 }
 
+// What the fold starts from: kLow is no maximum, and -inf logits give exp2(-inf) = 0.
+__device__ inline Top top_low() { return Top{kLow, kLowRef, 0.f, 0x7fffffff}; }
+
 // Fold n consecutive values starting at index v into t (values in index order).
 template <int N>
 __device__ inline void top_fold(Top& t, const float (&f)[N], int v) {
@@ -40,13 +43,9 @@ __device__ inline void top_fold(Top& t, const float (&f)[N], int v) {
         t.mL = nmL;
         t.idx = v + j0;
     }
-    // While t is empty (mL = -inf, only before the first finite value) the
-    // reference is the lowest finite float instead, so -inf logits give
-    // exp2(-inf) = 0 rather than -inf + inf: no branch on all -inf groups.
-    const float ref = fmaxf(t.mL, -3.402823466e38f);
     float e[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(f[j], kLog2e, -ref));
+    for (int j = 0; j < N; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(f[j], kLog2e, -t.mL));
 #pragma unroll
     for (int w = 1; w < N; w <<= 1)
 #pragma unroll
