@@ -504,7 +504,6 @@ mx4_still_kernel(MxArgs a, PackView pv, int n_units, int log_run) {
     live_rows(pv, 0, a.row_cap, live, none, TT * 16);
     if (!live) return;   // uniform over the workgroup
     const int lr = lane & 15, g = lane >> 4;
-    const int C = (a.K + 127) / 128;
     const int c0 = wave * CS;
 
     // ---- loads: lane l of op o has 16-byte piece i % (4 CS) of row i / (4 CS),
@@ -699,12 +698,17 @@ hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scale
     const int rows16 = (cap + 15) / 16;
     // x stationary: long outputs (16 tiles a CU), where the time to fetch x is small
     // beside the walk, K from 12 chunks to what the registers hold, 32 rows at most.
-    // M x N x K, this form and the ring: 1 x 131072 x 4096 56 and 105 us, 32 x 131072 x
-    // 4096 65 and 109; 1 x 65536 x 1536 14.3 and 15.4, 32 x 65536 x 1536 17.7 and 17.0.
-    // Outside: 1 x 16384 x 2048 7.3 and 6.3, 32 x 131072 x 1152 27.9 and 23.3, 64 x
-    // 157184 x 2048 56 and 58.
+    // M x N x K, this form and the ring: 1 x 131072 x 4096 55 and 105 us, 32 x 131072 x
+    // 4096 66 and 106; 1 x 65536 x 1536 15.1 and 15.0, 1 x 65536 x 2304 22.3 and 21.9.
+    // Outside: 1 x 16384 x 2048 7.3 and 6.3, 1 x 65536 x 1408 14.9 and 14.2, 64 x
+    // 157184 x 2048 56 and 58.  Two row tiles, and chunks that keep six or seven of the
+    // eight waves at work: 24 tiles a CU (32 x 65536 x 1536 18.7 and 18.0, 32 x 65536 x
+    // 2304 27.4 and 23.4, but 32 x 100000 x 1536 25.9 and 26.5, 32 x 157184 x 2304 54 and
+    // 55; whole, 32 x 65536 x 1920 21.1 and 22.9, 32 x 65536 x 3200 31.5 and 36.5).
     const int C = (K + 127) / 128;
-    if (C >= 12 && C <= 32 && rows16 <= 2 && tiles >= 16 * cu_count) {
+    const bool idle = C < 15 || (C > 16 && C < 23);
+    if (C >= 12 && C <= 32 && rows16 <= 2 &&
+        tiles >= (rows16 == 2 && idle ? 24 : 16) * cu_count) {
         auto still = [&](auto t, auto c, auto n) {
             constexpr int T = decltype(t)::value, S = decltype(c)::value, M = decltype(n)::value;
             // runs of four tiles, 128 bytes of a row of bf16 results: written by one
@@ -733,10 +737,10 @@ hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scale
     const long long want = 8LL * cu_count;     // one tile per wave
     if (units(TT) <= want / 2) {
         // the cheapest of T token tiles and KW waves to a tile: rounds of workgroups x
-        // (a start + stages x a stage's time, us, fitted to what all eight pairs take:
-        // 0.43 at (1, 2) to 1.1 at (4, 4)).  32 x 4096 x 4096: (1, 4) 6.3 us, (2, 8)
-        // 7.4, (4, 2) 15.6; 64 x 4096 x 4096: (2, 4) 8.0, (1, 2) 9.1, (4, 4) 11.0;
-        // 96 x 8192 x 4096: (4, 2) 16.6, (1, 2) 18.2, (2, 2) 21.0.
+        // (a start + stages x a stage's time, us: 0.43 at (1, 2) to 1.3 at (8, 2)).  Over
+        // nine shapes within 4% of the fastest of the ten pairs.  32 x 4096 x 4096: (1, 4)
+        // 6.4 us, (2, 8) 8.2, (4, 2) 14.8; 64 x 4096 x 4096: (2, 4) 8.1, (1, 2) 9.4, (4, 4)
+        // 11.6; 96 x 8192 x 4096: (4, 2) 17.7, (1, 2) 21.8, (2, 2) 22.6.
         int t = 1, kw = 2;
         double best = 1e30;
         for (int T : {1, 2, 4, 6, 8})
