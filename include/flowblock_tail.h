@@ -141,7 +141,7 @@ size_t fb_rules_workspace_bytes(const fb_pack* pack, int V);
  * keeps ws untouched in between, the pack and the request states as they were.
  *   st      device fb_req_state[B], as given to fb_pack_wavefronts
  *   tokens  device int32[B][T_max]; ids outside [0, V) are passed over
- *   rules   n_masks, masks and row_mask are not read
+ *   rules   what masks and row_mask point to is not read
  *   ws      device workspace of fb_rules_workspace_bytes bytes, 16-byte aligned */
 int fb_rules_build(const fb_logit_rules* rules, const fb_req_state* st,
                    const int32_t* tokens, int T_max, int V, const fb_pack* pack,
@@ -152,14 +152,16 @@ int fb_rules_build(const fb_logit_rules* rules, const fb_req_state* st,
  * the form fb_denoise_apply reads, so fb_rules_build + fb_vocab_reduce_rules
  * + fb_denoise_apply is fb_denoise_update on z'.  A row with nothing left (no
  * z' above -inf) has p = 0 and x_hat = -1; fb_denoise_apply never writes it.
- * Finite z' below -2^26 (masks of -1e9 or of the type's lowest value) count as
- * -2^26 here; z' are at most 2^26.
- *   logits  [row_cap][V], dtype FB_BF16 or FB_F32; an allowed entry is neither
- *           NaN nor +inf (others may hold anything)
+ * Finite z' at or below -2^26 (masks of -1e9 or of the type's lowest value)
+ * weigh nothing beside larger ones here, and count as equal, as -2^26, where
+ * there are no larger ones; z' are at most 2^26.
+ *   logits  [row_cap][V], dtype FB_BF16 or FB_F32, 16-byte aligned; an allowed
+ *           entry is neither NaN nor +inf (others may hold anything)
  *   conf, argmax  [row_cap] float32 and int32: p and x_hat of the live rows, or
  *           both NULL
  *   rules_ws  what fb_rules_build wrote for these rules, pack and V
- *   upd_ws  device workspace of fb_update_workspace_bytes(pack, V) bytes */
+ *   upd_ws  device workspace of fb_update_workspace_bytes(pack, V) bytes,
+ *           16-byte aligned */
 int fb_vocab_reduce_rules(const void* logits, int V, int dtype, const fb_pack* pack,
                           const fb_logit_rules* rules, const void* rules_ws,
                           size_t rules_ws_bytes, void* upd_ws, size_t upd_ws_bytes,
@@ -167,7 +169,8 @@ int fb_vocab_reduce_rules(const void* logits, int V, int dtype, const fb_pack* p
 
 /* The logits under the rules, z' rounded once to their type, for samplers of
  * the caller's own.
- *   logits, out  [row_cap][V], dtype FB_BF16 or FB_F32; out may be logits
+ *   logits, out  [row_cap][V], dtype FB_BF16 or FB_F32, 16-byte aligned; out
+ *           may be logits
  * The other arguments as above. */
 int fb_logits_rules(const void* logits, void* out, int V, int dtype,
                     const fb_pack* pack, const fb_logit_rules* rules,
