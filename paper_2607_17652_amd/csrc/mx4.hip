@@ -68,7 +68,8 @@ __device__ inline void live_rows(const PackView& pv, int r0, int row_cap, uint64
     const int lane = threadIdx.x & 63;
     const int r = r0 + lane;
     m0 = __ballot(lane < n && r < row_cap && pv.row_req[min(r, row_cap - 1)] >= 0);
-    m1 = n > 64 ? __ballot(r + 64 < row_cap && pv.row_req[min(r + 64, row_cap - 1)] >= 0) : 0;
+    m1 = n > 64 ? __ballot(lane + 64 < n && r + 64 < row_cap &&
+                           pv.row_req[min(r + 64, row_cap - 1)] >= 0) : 0;
 }
 
 // Four neighbouring results; those past N fall away.  Rows of an N that is no multiple
