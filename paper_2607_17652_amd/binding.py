@@ -491,12 +491,12 @@ def _refuse(t, dtype, n, name):
 
 def _octets(t, n, name):
     """The pointer of t, n bytes in elements of one byte, whatever they are called."""
+    if t.nbytes == n == t.numel() and t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
     if t.element_size() != 1:
         raise FlowBlockError(FB_E_INVAL, f"{name} holds {t.dtype}, not bytes")
     if t.numel() != n:
         raise FlowBlockError(FB_E_INVAL, f"{name} has {t.numel()} bytes, not {n}")
-    if t.is_contiguous() and t.is_cuda:
-        return t.data_ptr()
     return _refuse(t, None, n, name)
 
 
