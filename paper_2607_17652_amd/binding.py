@@ -1,4 +1,5 @@
-"""ctypes binding of libflowblock.so -- argument marshalling only.
+"""ctypes binding of libflowblock.so -- argument marshalling, and checks of what the
+library cannot see of the tail's tensors.
 
 Each function has the name of the C entry point it calls and takes torch
 tensors where the C call takes device pointers; every step of the work runs

@@ -14,9 +14,10 @@
 //             waves), and each wave's own codes and scales.  A wave owns NT
 //             16-column tiles; where the columns are few, KW waves share a
 //             tile, take the chunks of a stage in turn and join at the end.
-//             Many rows are bound by the matrix cores: 1024 x 16384 x 4096 107 us,
-//             1.29 PFLOP/s; 96 x 157184 x 2048 68 us, 0.91 PFLOP/s; 1 x 4096 x
-//             4096 5.1 us.  A large bf16 product reaches 1.13 PFLOP/s on this card.
+//             Many rows are bound by the matrix cores: 1024 x 16384 x 4096 100-107
+//             us, 1.29-1.37 PFLOP/s; 96 x 157184 x 2048 68-72 us, 0.86-0.91 PFLOP/s;
+//             1 x 4096 x 4096 5.1 us.  Large bf16 library products reach 1.13
+//             (8192^3) and 1.36 PFLOP/s (20416 x 157184 x 2048) on this card.
 // mx4_pair_kernel  more rows and a long output: codes two chunks at a time.
 // mx4_still_kernel  few rows and a long output: x stays in registers and the
 //             weights of whole rows stream by.
@@ -476,8 +477,8 @@ mx4_pair_kernel(MxArgs a, PackView pv, int n_groups) {
 // (TT 16-token tiles, CS chunks) in registers for the whole call, and the
 // workgroup walks units of NT 16-column tiles.  It reads a tile's rows whole, 16 KB
 // in one piece at K = 2048, where the ring above reads 64 bytes of many rows at a
-// time (which the memory serves at 4 TB/s at most): 1 x 157184 x 2048 35 us, 4.85
-// TB/s, and 44 us by the ring.  The partial sums of a tile join in LDS.
+// time (which the memory serves at 4 TB/s at most): 1 x 157184 x 2048 34.6 us, 4.95
+// TB/s, and 43 us by the ring.  The partial sums of a tile join in LDS.
 // DW: scales in dwords (K a multiple of 128 and scales 4-byte aligned).
 template <int TT, int CS, int NT, bool DW>
 struct MxStill {
@@ -783,8 +784,9 @@ hipError_t launch_mx4_linear(const void* x, const void* codes, const void* scale
     }
     // Codes two chunks at a time, while they and the sums fit the registers (beyond, at
     // 96 x 157184 x 2048 and five tiles, 70 us and more; the ring 69).  This form and
-    // the ring: 64 x 157184 x 2048 53 and 58 us, 128 x 157184 x 2048 90 and 97, 96 x
-    // 65536 x 4096 50 and 62, 128 x 65536 x 4096 61 and 76, 256 x 16384 x 4096 43 and 45.
+    // the ring: 64 x 157184 x 2048 52 and 58 us, 128 x 157184 x 2048 89 and 94, 96 x
+    // 65536 x 4096 53 and 63, 128 x 65536 x 4096 65 and 74, 512 x 16384 x 4096 60 and 67,
+    // 256 x 16384 x 4096 48 and 48.
     if (dw && K % 256 == 0 && TT >= 4 && nt > 1 && TT * nt <= 24) {
         auto pair = [&](auto tt, auto n) {
             constexpr int T = decltype(tt)::value, M = decltype(n)::value;
