@@ -1,5 +1,5 @@
 """ctypes binding of libflowblock.so -- argument marshalling, and checks of what the
-library cannot see of the tail's tensors.
+library cannot see of the tail's and the quantised cache's tensors.
 
 Each function has the name of the C entry point it calls and takes torch
 tensors where the C call takes device pointers; every step of the work runs
@@ -26,6 +26,7 @@ FB_DERR_STATE = 1
 FB_DERR_PAGE = 2
 FB_DERR_PLAN = 3
 FB_DERR_RULE = 4
+FB_DERR_SPAN = 5
 
 FB_F32 = 0
 FB_BF16 = 1
@@ -35,8 +36,11 @@ FB_PADDED = 1
 FB_EDIT_MASKED = 1
 FB_FORCE_PROGRESS = 2
 FB_SYNC_WINDOW = 4
+FB_MX4 = 4
+FB_MX8 = 8
 
 LAYOUTS = {"ragged": FB_RAGGED, "padded": FB_PADDED}
+PAIRINGS = {"halves": 0, "neighbours": 1}
 GATES = {"none": 0, "all": 1, "request": 2, "row": 3}
 
 # Every symbol include/*.h declares.
@@ -52,6 +56,8 @@ EXPORTS = [
     "fb_hbm_read_probe", "fb_hbm_copy_probe", "fb_denoise_update_noalloc",
     "fb_residual_norm", "fb_mx4_linear", "fb_rules_workspace_bytes", "fb_rules_build",
     "fb_vocab_reduce_rules", "fb_logits_rules",
+    "fb_rotary_axes", "fb_mx_write_window_kv", "fb_mx_read_kv",
+    "fb_mx_attention_workspace_bytes", "fb_mx_attention",
 ]
 FB_NOALLOC_SCRATCH_BYTES = 4 << 20
 FB_PROBE_BLOCKS = 2048
@@ -122,6 +128,18 @@ class fb_logit_rules(ctypes.Structure):
                 ("params", "bias_start", "bias_id", "bias_val", "masks", "row_mask")] + \
         [("n_bias", ctypes.c_int32), ("n_masks", ctypes.c_int32)]
     tensors = (None,) * 6       # make_rules: what the pointers belong to
+
+
+class fb_rotary(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("n_pairs", ctypes.c_int32),
+                ("pairing", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("freq", ctypes.c_double * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
+class fb_mx_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] + \
+        [("format", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+    tensors = (None,) * 4       # make_mx_cache: what the pointers belong to
 
 
 # numpy views of the device records
@@ -197,6 +215,15 @@ def lib():
                                             sz, vp, sz, vp, vp, vp]),
             "fb_logits_rules": (i32, [vp, vp, i32, i32, P(fb_pack), P(fb_logit_rules), vp, sz,
                                       vp]),
+            "fb_rotary_axes": (i32, [vp, vp, vp, vp, vp, P(fb_pack), P(fb_attn_shape),
+                                     P(fb_rotary), vp]),
+            "fb_mx_write_window_kv": (i32, [vp, vp, P(fb_mx_cache), vp, P(fb_pack),
+                                            P(fb_attn_shape), vp]),
+            "fb_mx_read_kv": (i32, [P(fb_mx_cache), vp, vp, i32, vp, vp, P(fb_pack),
+                                    P(fb_attn_shape), vp]),
+            "fb_mx_attention_workspace_bytes": (sz, [P(fb_pack), P(fb_attn_shape)]),
+            "fb_mx_attention": (i32, [vp, P(fb_mx_cache), vp, P(fb_pack), P(fb_attn_shape), vp,
+                                      vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -610,6 +637,92 @@ def fb_logits_rules(logits, out, pack, rules, rules_ws, stream=None):
                                  _dtype_code(logits), pack.handle, _rules(rules, pack, V),
                                  _space(rules_ws, "rules_ws"), rules_ws.nbytes,
                                  _stream(stream)))
+
+
+# ---------------------------------------------------- the quantised cache
+# Checked as the tail's calls are: type, density and size of every tensor against the
+# pack, the shape and the cache.
+def make_rotary(freq, axis, pairing="halves"):
+    """Pair j turns by positions[axis[j]][row] * freq[j]; its elements are j and
+    len(freq) + j ("halves") or 2j and 2j + 1 ("neighbours")."""
+    n = len(freq)
+    if n != len(axis) or not 1 <= n <= 64:
+        raise FlowBlockError(FB_E_INVAL, f"{n} frequencies and {len(axis)} axes: need 1 .. 64 of "
+                                         "each")
+    if min(axis) < 0 or max(axis) > 7:
+        raise FlowBlockError(FB_E_INVAL, "axes are 0 .. 7")
+    r = fb_rotary(max(axis) + 1, n, PAIRINGS[pairing] if isinstance(pairing, str) else pairing)
+    r.freq[:n], r.axis[:n] = freq, axis
+    return r
+
+
+def rotary_sections(head_dim, sections, base=10000.0):
+    """(freq, axis) of make_rotary for heads whose first sections[0] pairs turn by axis 0,
+    the next sections[1] by axis 1, and so on, pair j at base^(-2j/head_dim)."""
+    axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    return [base ** (-2.0 * j / head_dim) for j in range(len(axis))], axis
+
+
+def fb_rotary_axes(q_in, q_out, k_in, k_out, positions, pack, shape, rotary, stream=None):
+    """q [row_cap, Hq, d] and k [row_cap, Hkv, d] (either pair may be None) turned by
+    positions int32 [n_axes, row_cap]."""
+    t, row = _type(shape.dtype), pack.row_cap * shape.head_dim
+    nq, nk = row * shape.Hq, row * shape.Hkv
+    _check(lib().fb_rotary_axes(_dense(q_in, t, nq, "q_in"), _dense(q_out, t, nq, "q_out"),
+                                _dense(k_in, t, nk, "k_in"), _dense(k_out, t, nk, "k_out"),
+                                _dense(positions, _type(FB_I32), rotary.n_axes * pack.row_cap,
+                                       "positions"),
+                                pack.handle, shape, rotary, _stream(stream)))
+
+
+def make_mx_cache(format, k_codes, k_scales, v_codes, v_scales):
+    """format FB_MX4 or FB_MX8; codes uint8 [num_pages, Hkv, page_size, d * format / 8],
+    scales uint8 [num_pages, Hkv, page_size, d / 32].  Keeps its tensors alive."""
+    t = (k_codes, k_scales, v_codes, v_scales)
+    names = ("k_codes", "k_scales", "v_codes", "v_scales")
+    c = fb_mx_cache(*(_octets(x, x.numel(), n) for x, n in zip(t, names)), format)
+    c.tensors = t
+    return c
+
+
+def _mx_cache(cache, page_table, pack, shape):
+    """The cache and the page table's pointer, which fit the shape."""
+    slots = shape.num_pages * shape.Hkv * shape.page_size
+    sizes = (slots * shape.head_dim * cache.format // 8, slots * (shape.head_dim // 32))
+    for t, n, name in zip(cache.tensors, sizes * 2, ("k_codes", "k_scales", "v_codes", "v_scales")):
+        if t is not None and t.numel() < n:
+            _refuse(t, None, n, name)
+    return cache, _dense(page_table, _type(FB_I32), pack.B * shape.max_pages, "page_table")
+
+
+def fb_mx_write_window_kv(k_new, v_new, cache, page_table, pack, shape, stream=None):
+    t, n = _type(shape.dtype), pack.row_cap * shape.Hkv * shape.head_dim
+    _check(lib().fb_mx_write_window_kv(_dense(k_new, t, n, "k_new"), _dense(v_new, t, n, "v_new"),
+                                       *_mx_cache(cache, page_table, pack, shape), pack.handle,
+                                       shape, _stream(stream)))
+
+
+def fb_mx_read_kv(cache, page_table, spans, k_out, v_out, pack, shape, stream=None):
+    """spans int32 [B, 2]: first position and count; k_out, v_out [B, T, Hkv, d] (one may
+    be None)."""
+    out = k_out if k_out is not None else v_out
+    T = 0 if out is None else out.shape[1]
+    t, n = _type(shape.dtype), pack.B * T * shape.Hkv * shape.head_dim
+    _check(lib().fb_mx_read_kv(*_mx_cache(cache, page_table, pack, shape),
+                               _dense(spans, _type(FB_I32), 2 * pack.B, "spans"), T,
+                               _dense(k_out, t, n, "k_out"), _dense(v_out, t, n, "v_out"),
+                               pack.handle, shape, _stream(stream)))
+
+
+def fb_mx_attention_workspace_bytes(pack, shape):
+    return int(lib().fb_mx_attention_workspace_bytes(pack.handle, shape))
+
+
+def fb_mx_attention(q, cache, page_table, pack, shape, out, ws, stream=None):
+    t, n = _type(shape.dtype), pack.row_cap * shape.Hq * shape.head_dim
+    _check(lib().fb_mx_attention(_dense(q, t, n, "q"), *_mx_cache(cache, page_table, pack, shape),
+                                 pack.handle, shape, _dense(out, t, n, "out"), _space(ws, "ws"),
+                                 ws.nbytes, _stream(stream)))
 
 
 # ------------------------------------------------------ multi-step loop

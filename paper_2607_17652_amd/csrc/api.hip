@@ -9,6 +9,7 @@
 
 #include <mutex>
 
+#include "cache.h"
 #include "internal.h"
 
 namespace {
@@ -63,7 +64,8 @@ int check_pack(const fb_pack* p) {
     return FB_OK;
 }
 
-int check_shape(const fb_pack* p, const fb_attn_shape* sh) {
+// What every cache wants of a shape.
+int check_heads_and_pages(const fb_attn_shape* sh) {
     if (!sh) return fail(FB_E_INVAL, "shape is NULL");
     if (sh->Hq < 1 || sh->Hkv < 1 || sh->Hq % sh->Hkv)
         return fail(FB_E_INVAL, "need Hq >= 1, Hkv >= 1 and Hq %% Hkv == 0 (got %d, %d)",
@@ -74,18 +76,24 @@ int check_shape(const fb_pack* p, const fb_attn_shape* sh) {
         return fail(FB_E_UNSUPPORTED, "dtype %d not supported", sh->dtype);
     if (!is_pow2(sh->page_size))
         return fail(FB_E_INVAL, "page_size %d is not a power of two", sh->page_size);
-    if (sh->dtype == FB_BF16 && sh->page_size < 8)
-        return fail(FB_E_UNSUPPORTED, "bf16 needs page_size >= 8 (got %d)", sh->page_size);
     if (sh->max_pages < 1 || sh->num_pages < 1)
         return fail(FB_E_INVAL, "max_pages and num_pages must be >= 1");
+    if (isnan(sh->sm_scale) || isinf(sh->sm_scale))
+        return fail(FB_E_INVAL, "sm_scale is not finite");
+    return FB_OK;
+}
+
+int check_shape(const fb_pack* p, const fb_attn_shape* sh) {
+    const int rc = check_heads_and_pages(sh);
+    if (rc) return rc;
+    if (sh->dtype == FB_BF16 && sh->page_size < 8)
+        return fail(FB_E_UNSUPPORTED, "bf16 needs page_size >= 8 (got %d)", sh->page_size);
     if (sh->kv_split < 0 || sh->kv_split % 32)
         return fail(FB_E_INVAL, "kv_split %d must be 0 or a positive multiple of 32",
                     sh->kv_split);
     const size_t elt = sh->dtype == FB_BF16 ? 2 : 4;
     if ((size_t)p->bl * sh->head_dim * elt > 65536)
         return fail(FB_E_UNSUPPORTED, "bl*head_dim too large for the KV staging buffer");
-    if (isnan(sh->sm_scale) || isinf(sh->sm_scale))
-        return fail(FB_E_INVAL, "sm_scale is not finite");
     return FB_OK;
 }
 
@@ -880,6 +888,138 @@ int fb_decode_loop(const fb_loop_args* a, int max_steps, int check_every, int us
     cleanup();
     if (steps_out) *steps_out = enq;
     if (done_out) *done_out = done;
+    return ok();
+}
+
+// ---- the quantised cache (flowblock_cache.h) -------------------------------
+
+namespace {
+
+static size_t elt_bytes(const fb_attn_shape* sh) { return sh->dtype == FB_BF16 ? 2 : 4; }
+
+static int check_mx_cache(const fb_mx_cache* c, const int32_t* page_table) {
+    if (!c) return fail(FB_E_INVAL, "cache is NULL");
+    if (c->format != FB_MX4 && c->format != FB_MX8)
+        return fail(FB_E_UNSUPPORTED, "cache format %d is neither FB_MX4 nor FB_MX8", c->format);
+    if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales || !page_table)
+        return fail(FB_E_INVAL, "a cache pointer or the page table is NULL");
+    if (!aligned16(c->k_codes) || !aligned16(c->v_codes))
+        return fail(FB_E_INVAL, "codes must be 16-byte aligned");
+    if (!aligned(page_table, 4)) return fail(FB_E_INVAL, "page_table must be 4-byte aligned");
+    return FB_OK;
+}
+
+}  // namespace
+
+int fb_rotary_axes(const void* q_in, void* q_out, const void* k_in, void* k_out,
+                   const int32_t* positions, const fb_pack* pack, const fb_attn_shape* sh,
+                   const fb_rotary* rotary, void* stream) {
+    int rc = check_pack(pack);
+    if (rc) return rc;
+    rc = check_heads_and_pages(sh);
+    if (rc) return rc;
+    if (!rotary) return fail(FB_E_INVAL, "rotary is NULL");
+    if (rotary->n_axes < 1 || rotary->n_axes > 8)
+        return fail(FB_E_INVAL, "n_axes %d outside [1, 8]", rotary->n_axes);
+    if (rotary->n_pairs < 1 || rotary->n_pairs > sh->head_dim / 2)
+        return fail(FB_E_INVAL, "n_pairs %d outside [1, head_dim/2]", rotary->n_pairs);
+    if (rotary->pairing != FB_PAIR_HALVES && rotary->pairing != FB_PAIR_NEIGHBOURS)
+        return fail(FB_E_INVAL, "pairing %d is not an FB_PAIR_*", rotary->pairing);
+    for (int j = 0; j < rotary->n_pairs; ++j) {
+        if (rotary->axis[j] >= rotary->n_axes)
+            return fail(FB_E_INVAL, "pair %d turns by axis %d of %d", j, rotary->axis[j],
+                        rotary->n_axes);
+        if (isnan(rotary->freq[j]) || isinf(rotary->freq[j]))
+            return fail(FB_E_INVAL, "the frequency of pair %d is not finite", j);
+    }
+    if (!q_in != !q_out || !k_in != !k_out)
+        return fail(FB_E_INVAL, "an input and its output go together");
+    if (!q_in && !k_in) return fail(FB_E_INVAL, "neither queries nor keys");
+    if (!positions || !aligned(positions, 4))
+        return fail(FB_E_INVAL, "positions must be a 4-byte aligned pointer");
+    if (!aligned16(q_in) || !aligned16(q_out) || !aligned16(k_in) || !aligned16(k_out))
+        return fail(FB_E_INVAL, "q and k pointers must be 16-byte aligned");
+    const size_t row = (size_t)pack->row_cap * sh->head_dim * elt_bytes(sh);
+    const size_t nq = row * sh->Hq, nk = row * sh->Hkv;
+    if ((q_out != q_in && overlap(q_out, nq, q_in, nq)) ||
+        (k_out != k_in && overlap(k_out, nk, k_in, nk)) || overlap(q_out, nq, k_in, nk) ||
+        overlap(k_out, nk, q_in, nq) || overlap(q_out, nq, k_out, nk))
+        return fail(FB_E_INVAL, "outputs overlap each other or an input");
+    hipError_t e = fb::launch_rotary(q_in, q_out, k_in, k_out, positions, pack, sh, rotary,
+                                     (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "rotary launch");
+    return ok();
+}
+
+int fb_mx_write_window_kv(const void* k_new, const void* v_new, const fb_mx_cache* cache,
+                          const int32_t* page_table, const fb_pack* pack,
+                          const fb_attn_shape* sh, void* stream) {
+    int rc = check_pack(pack);
+    if (rc) return rc;
+    rc = check_heads_and_pages(sh);
+    if (rc) return rc;
+    rc = check_mx_cache(cache, page_table);
+    if (rc) return rc;
+    if (!k_new || !v_new) return fail(FB_E_INVAL, "a tensor pointer is NULL");
+    if (!aligned16(k_new) || !aligned16(v_new))
+        return fail(FB_E_INVAL, "K/V pointers must be 16-byte aligned");
+    hipError_t e = fb::launch_mx_write(k_new, v_new, cache, page_table, pack, sh,
+                                       (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "quantised KV write launch");
+    return ok();
+}
+
+int fb_mx_read_kv(const fb_mx_cache* cache, const int32_t* page_table, const int32_t* spans, int T,
+                  void* k_out, void* v_out, const fb_pack* pack, const fb_attn_shape* sh,
+                  void* stream) {
+    int rc = check_pack(pack);
+    if (rc) return rc;
+    rc = check_heads_and_pages(sh);
+    if (rc) return rc;
+    rc = check_mx_cache(cache, page_table);
+    if (rc) return rc;
+    if (T < 1) return fail(FB_E_INVAL, "T must be >= 1");
+    if (!spans || !aligned(spans, 4))
+        return fail(FB_E_INVAL, "spans must be a 4-byte aligned pointer");
+    if (!k_out && !v_out) return fail(FB_E_INVAL, "neither k_out nor v_out");
+    if (!aligned16(k_out) || !aligned16(v_out))
+        return fail(FB_E_INVAL, "k_out and v_out must be 16-byte aligned");
+    const size_t nb = (size_t)pack->B * T * sh->Hkv * sh->head_dim * elt_bytes(sh);
+    if (overlap(k_out, nb, v_out, nb)) return fail(FB_E_INVAL, "k_out and v_out overlap");
+    hipError_t e = fb::launch_mx_read(cache, page_table, spans, T, k_out, v_out, pack, sh,
+                                      cu_count(), (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "quantised KV read launch");
+    return ok();
+}
+
+size_t fb_mx_attention_workspace_bytes(const fb_pack* pack, const fb_attn_shape* sh) {
+    if (check_pack(pack) || check_heads_and_pages(sh)) return 0;
+    return fb::mx_attention_sizes(pack, sh, cu_count()).total;
+}
+
+int fb_mx_attention(const void* q, const fb_mx_cache* cache, const int32_t* page_table,
+                    const fb_pack* pack, const fb_attn_shape* sh, void* out, void* ws,
+                    size_t ws_bytes, void* stream) {
+    int rc = check_pack(pack);
+    if (rc) return rc;
+    rc = check_heads_and_pages(sh);
+    if (rc) return rc;
+    rc = check_mx_cache(cache, page_table);
+    if (rc) return rc;
+    if (!q || !out) return fail(FB_E_INVAL, "a tensor pointer is NULL");
+    if (!aligned16(q) || !aligned16(out))
+        return fail(FB_E_INVAL, "q and out must be 16-byte aligned");
+    const size_t nb = (size_t)pack->row_cap * sh->Hq * sh->head_dim * elt_bytes(sh);
+    if (out != q && overlap(q, nb, out, nb))
+        return fail(FB_E_INVAL, "out overlaps q without being it");
+    const fb::MxAttnSizes z = fb::mx_attention_sizes(pack, sh, cu_count());
+    if (!ws || ws_bytes < z.total)
+        return fail(FB_E_WORKSPACE, "attention workspace has %zu bytes, needs %zu", ws_bytes,
+                    z.total);
+    if (!aligned16(ws)) return fail(FB_E_INVAL, "workspace must be 16-byte aligned");
+    hipError_t e = fb::launch_mx_attention(q, cache, page_table, pack, sh, out, ws, z,
+                                           (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "quantised attention launch");
     return ok();
 }
 

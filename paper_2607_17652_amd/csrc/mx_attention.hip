@@ -1,0 +1,866 @@
+// Windowed block-causal attention (Sec. 4.1; Eq. 5 per packed row) over a
+// quantised cache: keys and values in E2M1 or E4M3 with a power-of-two scale per
+// 32 channels.
+//
+// Such a value has at most four significant bits and a power of two, so bf16
+// holds it exactly: the products run on v_mfma_f32_32x32x16_bf16 and add up in
+// float32.  (The instructions that multiply codes and scales directly were
+// measured too: their sums are off by up to 2^-12.5 of the sum of the products'
+// magnitudes, where a float32 addition is off by 2^-24.)
+//
+// Work.  A unit is (request, KV head, group of query rows): the request's rows
+// are its window's (position, head of the KV head's group) pairs, position
+// major, so a group may span several blocks, which share one pass over the
+// prefix; the blocks differ in their last keys only, by a mask per row.  The
+// units' key tiles (32 keys), with a few more for a unit's start and end, form
+// one line, cut into equal shares, one for each workgroup: no list is made, a
+// workgroup finds its place in the line from the requests' windows alone.  A
+// unit that a cut divides is merged afterwards.
+//   mx_wide_kernel   groups of 128 rows, 32 to a wave; the waves share a key
+//                    tile, which they turn into bf16 in LDS
+//   mx_few_kernel    requests of at most 32 rows (single tokens among them):
+//                    the waves take key tiles in turn, each for all rows, and
+//                    join at the end; no tile is shared, so no wave waits
+//   mx_merge_kernel  the divided units' pieces, by their log-sum-exps
+//
+// S^T = K Q^T leaves in lane l the scores of query row l % 32 and keys
+// 8 (x / 4) + 4 (l / 32) + x % 4, x < 16.  The product O^T += V^T P^T takes the
+// keys in that order: V is read transposed (ds_read_b64_tr_b16, four keys at a
+// time), so P goes from one product into the other without an exchange.
+// fp32: queries and weights are split into three bf16 parts, which hold all 24
+// bits, so there are three products each.
+#include <type_traits>
+
+#include "cache.h"
+
+namespace fb {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kTile = 32;              // keys
+constexpr int kWideRows = 128, kFewRows = 32;
+constexpr int kStart = 5;              // what a unit's start and end cost, in key tiles
+constexpr int kLeastShare = 8;         // of a workgroup
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kRescaleSlack = 8.0f;  // the running maximum may lag by 2^8
+
+struct MxArgs {
+    const void* q;
+    const uint8_t *kc, *ks, *vc, *vs;
+    const int32_t* page_table;
+    void* out;
+    int32_t* head;     // [0]: workgroups with a share
+    int32_t* rec;      // [wgs][8]: the unit whose first piece the workgroup made
+    float* part_o;     // [2 wgs][rows][D]
+    float* part_lse;   // [2 wgs][rows]
+    int Hq, Hkv, g, bl, B, W_max, row_cap, wgs, ps_shift, max_pages, num_pages;
+    float scale_log2;
+};
+enum RecField { kRRow0 = 0, kRHead, kRFirst, kRRows, kRPieces, kRecInts = 8 };
+
+// ----------------------------------------------------------- the shares ---
+// A request's part of the line.
+struct Req {
+    int b, row0, o, rows, groups;
+    int len;           // of one KV head
+};
+
+// A piece of a unit: key tiles [k0, k1) of kt.
+struct Piece {
+    int head, group, kt, k0, k1;
+    int first, more;   // partial slot (-1: the whole unit), pieces of a unit that begins here
+};
+
+template <int ROWS>
+__device__ inline int group_tiles(const MxArgs& a, const Req& r, int group) {
+    const int last = min((group + 1) * ROWS, r.rows) - 1;
+    return (r.o + (last / (a.g * a.bl) + 1) * a.bl + kTile - 1) / kTile;
+}
+
+// Request b; `report`: an unreachable page is recorded.
+template <int ROWS>
+__device__ inline Req request(const MxArgs& a, const PackView& pv, int b, bool report) {
+    Req r{b, 0, 0, 0, 0, 0};
+    const int w = pv.req_w[b], row0 = pv.req_row0[b];
+    if (w <= 0 || w > a.W_max || row0 < 0 || row0 > a.row_cap - w * a.bl) return r;
+    r.row0 = row0;
+    r.o = pv.row_pos[row0];
+    if ((long long)r.o + (long long)w * a.bl > ((long long)a.max_pages << a.ps_shift) || r.o < 0) {
+        if (report) record_error(pv.hdr, b, FB_DERR_PAGE);
+        return r;
+    }
+    r.rows = w * a.bl * a.g;
+    r.groups = (r.rows + ROWS - 1) / ROWS;
+    for (int i = 0; i < r.groups; ++i) r.len += group_tiles<ROWS>(a, r, i) + kStart;
+    return r;
+}
+
+// The walk of a workgroup along its share.
+template <int ROWS>
+struct Walk {
+    long long at, end;    // place in the line of the present unit, end of the share
+    long long share;
+    int index, head, group;
+    int skip;             // place of the share's start in its first unit
+    Req r;
+
+    // The cut at place x of a unit of kt tiles, in its tiles: what is left on
+    // either side is worth a piece.
+    __device__ inline int least() const { return (int)max(2LL, share / 16); }
+    __device__ inline int cut(long long x, int kt) const {
+        const int k = (int)max(0LL, min(x - kStart, (long long)kt)), m = least();
+        return k < m ? 0 : kt - k < m ? kt : k;
+    }
+
+    // All threads of the workgroup; false if it has no share.
+    __device__ bool begin(const MxArgs& a, const PackView& pv) {
+        __shared__ long long wave_sum[kThreads / 64];
+        __shared__ long long found[2];
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int per = (a.B + kThreads - 1) / kThreads;
+        long long mine = 0;
+        for (int b = tid * per; b < min((tid + 1) * per, a.B); ++b)
+            mine += (long long)a.Hkv * request<ROWS>(a, pv, b, blockIdx.x == 0).len;
+        long long sum = mine;                 // inclusive over the threads
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const long long x = __shfl_up(sum, off, 64);
+            if (lane >= off) sum += x;
+        }
+        if (lane == 63) wave_sum[wave] = sum;
+        __syncthreads();
+        long long total = 0;
+#pragma unroll
+        for (int i = 0; i < kThreads / 64; ++i) {
+            if (i < wave) sum += wave_sum[i];
+            total += wave_sum[i];
+        }
+        share = max((total + a.wgs - 1) / a.wgs, (long long)(kLeastShare + kStart));
+        const int busy = (int)((total + share - 1) / share);
+        // Neighbours in the line read the same keys, so they belong on one XCD:
+        // workgroups go to the eight in turn.
+        const int each = (busy + 7) / 8;
+        index = blockIdx.x % 8 * each + blockIdx.x / 8;
+        if (blockIdx.x == 0 && tid == 0) a.head[0] = busy;
+        if (blockIdx.x / 8 >= each || index >= busy) return false;
+        const long long p = index * share;
+        end = p + share;
+        if (sum > p && sum - mine <= p) {
+            // the request that holds p is one of this thread's
+            long long before = sum - mine;
+            int b = tid * per;
+            for (;; ++b) {
+                const long long len = (long long)a.Hkv * request<ROWS>(a, pv, b, false).len;
+                if (before + len > p) break;
+                before += len;
+            }
+            found[0] = b;
+            found[1] = before;
+        }
+        __syncthreads();
+        r = request<ROWS>(a, pv, (int)found[0], false);
+        at = found[1];
+        head = (int)((p - at) / r.len);
+        at += (long long)head * r.len;
+        group = 0;
+        for (;;) {
+            const int len = group_tiles<ROWS>(a, r, group) + kStart;
+            if (at + len > p) break;
+            at += len;
+            ++group;
+        }
+        skip = (int)(p - at);
+        return true;
+    }
+
+    // The next piece of the share; false past its last one.
+    __device__ bool next(const MxArgs& a, const PackView& pv, Piece& w) {
+        for (;;) {
+            if (at >= end) return false;
+            while (r.len == 0 || head >= a.Hkv) {
+                if (r.b + 1 >= a.B) return false;
+                r = request<ROWS>(a, pv, r.b + 1, false);
+                head = 0;
+            }
+            w.head = head;
+            w.group = group;
+            w.kt = group_tiles<ROWS>(a, r, group);
+            w.k0 = cut(skip, w.kt);
+            const int len = w.kt + kStart;
+            w.k1 = end - at >= len ? w.kt : cut(end - at, w.kt);
+            w.first = -1;
+            w.more = 0;
+            if (w.k0 > 0) w.first = 2 * index;
+            else if (w.k1 < w.kt && w.k1 > 0) {
+                // cuts at m .. kt - m tiles of this unit, this share's end the first
+                const long long last = (at + kStart + w.kt - least()) / share;
+                w.first = 2 * index + 1;
+                w.more = (int)(last - index) + 1;
+            }
+            at += len;
+            skip = 0;
+            if (++group == r.groups) group = 0, ++head;
+            if (w.k0 < w.k1) return true;
+        }
+    }
+};
+
+// ------------------------------------------------------------- operands ---
+// The three bf16 parts of a float: two cut off, so that each rest is exact and
+// the third holds what is left.
+__device__ inline void split3(float x, __bf16 (&p)[3]) {
+    const uint32_t hi = __float_as_uint(x) & 0xffff0000u;
+    const float r = x - __uint_as_float(hi);
+    const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
+    p[0] = __builtin_bit_cast(__bf16, (uint16_t)(hi >> 16));
+    p[1] = __builtin_bit_cast(__bf16, (uint16_t)(mid >> 16));
+    p[2] = (__bf16)(r - __uint_as_float(mid));
+}
+
+template <typename T>
+constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+
+// Eight query elements as an operand; zeros where there is no row.
+__device__ inline void query8(const uint16_t* p, bool ok, bf16x8 (&f)[1]) {
+    f[0] = ok ? *reinterpret_cast<const bf16x8*>(p) : bf16x8{};
+}
+__device__ inline void query8(const float* p, bool ok, bf16x8 (&f)[3]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        __bf16 s[3];
+        split3(ok ? p[i] : 0.f, s);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) f[k][i] = s[k];
+    }
+}
+
+__device__ inline void store4(uint16_t* p, float a, float b, float c, float d) {
+    const __bf16 v[4] = {(__bf16)a, (__bf16)b, (__bf16)c, (__bf16)d};
+    *reinterpret_cast<u32x2*>(p) = *reinterpret_cast<const u32x2*>(v);
+}
+__device__ inline void store4(float* p, float a, float b, float c, float d) {
+    *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
+
+// Where the 16-byte piece c of row r of a [32][D] bf16 tile lies in LDS, in
+// elements.  Free of bank conflicts are so: sixteen rows' same piece (key
+// operands; sixteen lanes a step); four neighbouring rows' same 64 bytes (value
+// operands, read transposed); two rows' alternate pieces (the stores of a tile
+// at D = 128, eight threads to a row).
+template <int D>
+__device__ inline int swz(int r, int c) {
+    if constexpr (D == 128) return r * D + ((c ^ ((r & 3) << 2 | (((r >> 2) & 3) ^ (r & 1)))) * 8);
+    else if constexpr (D == 64) return r * D + ((c ^ (((r >> 1) & 1) << 2 | ((r >> 2) & 3))) * 8);
+    else return r * D + ((c ^ ((r >> 2) & 3)) * 8);
+}
+
+// Values of column l % 16 and four neighbouring rows: lane i of each sixteen
+// gives the address of row i / 4, columns 4 (i % 4) ...
+__device__ inline s16x4 read_tr(const uint16_t* p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4*)(p));
+}
+
+// max over the lanes l and l + 32, which share a query row
+__device__ inline float half_max(float x) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                     false);
+    return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+
+// N bytes of codes as dwords.
+template <int N>
+__device__ inline void load_codes(const uint8_t* p, uint32_t* q) {
+    if constexpr (N == 2) q[0] = *reinterpret_cast<const uint16_t*>(p);
+    else if constexpr (N == 4) q[0] = *reinterpret_cast<const uint32_t*>(p);
+    else if constexpr (N == 8) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        q[0] = x[0], q[1] = x[1];
+    } else {
+#pragma unroll
+        for (int j = 0; j < N / 16; ++j) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(p + 16 * j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[4 * j + i] = x[i];
+        }
+    }
+}
+
+// Eight values from their codes (BITS / 4 dwords), zeros unless ok.
+template <int BITS>
+__device__ inline u32x4 eight_values(const uint32_t* q, float scale, bool ok) {
+    bf16x2 v[4];
+#pragma unroll
+    for (int i = 0; i < BITS / 4; ++i) mx_dword<BITS>(q[i], scale, v + i * (16 / BITS));
+    return u32x4{ok ? __builtin_bit_cast(uint32_t, v[0]) : 0u, ok ? __builtin_bit_cast(uint32_t, v[1]) : 0u,
+                 ok ? __builtin_bit_cast(uint32_t, v[2]) : 0u, ok ? __builtin_bit_cast(uint32_t, v[3]) : 0u};
+}
+
+// --------------------------------------------------------- online softmax ---
+// A wave's 32 query rows: lane l has row l % 32, half of its scores and of its
+// result's channels.
+template <int D, typename T>
+struct Rows {
+    static constexpr int KK = D / 16, DT = D / 32, NP = kParts<T>;
+    bf16x8 qf[KK][NP];
+    floatx16 o[DT];
+    float m_sub;      // what the scores are taken relative to, log2 domain
+    float thr;        // score above which it moves; -inf: no score above -inf yet
+    float l;          // this lane's share of the denominator
+    int seen;         // keys that the row sees
+
+    __device__ inline void clear() {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] = floatx16{};
+        m_sub = l = 0.f;
+        thr = -INFINITY;
+    }
+
+    // Scores into P^T and the running statistics; keys from `left` on (of the
+    // lane's row) are not seen.
+    __device__ inline void softmax(floatx16& s, float scale, int left, bool masked,
+                                   bf16x8 (&pb)[2][NP]) {
+        const int h = (threadIdx.x >> 5) & 1;
+        if (masked)
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+                if (8 * (x >> 2) + 4 * h + (x & 3) >= left) s[x] = -INFINITY;
+        float mx = s[0];
+#pragma unroll
+        for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x]);
+        mx = half_max(mx);
+        const bool need = mx > thr;
+        if (__any(need)) {
+            const float m_new = need ? mx * scale : m_sub;
+            // (the first time there is nothing to scale, and 2^(0 - m) may pass the range)
+            const float alpha = thr == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_sub - m_new);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[dt][x] *= alpha;
+            l *= alpha;
+            m_sub = m_new;
+            if (need) thr = mx + kRescaleSlack / scale;
+        }
+        // bf16: the weights are rounded for the product, and the denominator sums
+        // the rounded ones, so that the rounding cancels where values agree
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[x], scale, -m_sub));
+            if constexpr (NP == 1) {
+                pb[x >> 3][0][x & 7] = (__bf16)p;
+            } else {
+                __bf16 part[3];
+                split3(p, part);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) pb[x >> 3][k][x & 7] = part[k];
+                l += p;
+            }
+        }
+        if constexpr (NP == 1) {
+            const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+            for (int x = 0; x < 8; x += 2) {
+                l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[0][0][x], pb[0][0][x + 1]}, one, l, false);
+                l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[1][0][x], pb[1][0][x + 1]}, one, l, false);
+            }
+        }
+    }
+
+    // O^T += V^T P^T with V the tile at vt.
+    __device__ inline void add_values(const uint16_t* vt, const bf16x8 (&pb)[2][NP]) {
+        const int lane = threadIdx.x & 63, h = lane >> 5;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                // slots 8 h ...: keys 16 t + 4 h .. + 3, then 16 t + 8 + 4 h .. + 3
+                const int row = 16 * t + 4 * h + (lane & 15) / 4;
+                const int piece = dt * 4 + (lane & 16) / 8 + (lane & 3) / 2, in = (lane & 1) * 4;
+                union {
+                    s16x4 part[2];
+                    bf16x8 v;
+                } f;
+                f.part[0] = read_tr(vt + swz<D>(row, piece) + in);
+                f.part[1] = read_tr(vt + swz<D>(row + 8, piece) + in);
+#pragma unroll
+                for (int k = 0; k < NP; ++k)
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pb[t][k], o[dt], 0, 0, 0);
+            }
+    }
+
+    // Values of NaN scales in a tile that not every row sees were staged as zeros:
+    // the rows that do see them get their NaN here.
+    __device__ inline void spoil(const MxArgs& a, const int32_t* pt, int head, int key0, int end) {
+        for (int key = key0; key < min(key0 + kTile, end); ++key) {
+            const int page = pt[key >> a.ps_shift];
+            if ((unsigned)page >= (unsigned)a.num_pages) continue;
+            const uint8_t* s = a.vs + ((((size_t)page * a.Hkv + head) << a.ps_shift) +
+                                       (key & ((1 << a.ps_shift) - 1))) * DT;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                if (s[dt] == 255 && key < seen)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) o[dt][x] = __uint_as_float(0x7fc00000u);
+        }
+    }
+
+    // The rows' results, or their piece's.
+    __device__ inline void store(const MxArgs& a, const Req& r, const Piece& w, int r_local,
+                                 int row_stride) {
+        const int h = (threadIdx.x >> 5) & 1;
+        const float sum = l + __shfl_xor(l, 32, 64);
+        const int row = w.group * row_stride + r_local;
+        if (row >= r.rows) return;
+        // a piece that the row sees nothing of adds nothing to it
+        const float inv = w.first >= 0 && sum == 0.f ? 0.f : 1.0f / sum;
+        T* dst = static_cast<T*>(a.out) +
+                 ((size_t)(r.row0 + row / a.g) * a.Hq + w.head * a.g + row % a.g) * D;
+        const size_t slot = (size_t)(w.first < 0 ? 0 : w.first) * row_stride + r_local;
+        float* po = a.part_o + slot * D;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int x = 0; x < 16; x += 4) {
+                const int d = dt * 32 + x * 2 + h * 4;
+                const float v0 = o[dt][x] * inv, v1 = o[dt][x + 1] * inv;
+                const float v2 = o[dt][x + 2] * inv, v3 = o[dt][x + 3] * inv;
+                if (w.first < 0) store4(dst + d, v0, v1, v2, v3);
+                else store4(po + d, v0, v1, v2, v3);
+            }
+        if (w.first >= 0 && h == 0) a.part_lse[slot] = m_sub + __log2f(sum);
+    }
+};
+
+__device__ inline void store_record(const MxArgs& a, int index, const Req& r, const Piece& w,
+                                    int rows) {
+    int32_t* rec = a.rec + (size_t)index * kRecInts;
+    rec[kRRow0] = r.row0;
+    rec[kRHead] = w.head;
+    rec[kRFirst] = w.group * rows;
+    rec[kRRows] = min(rows, r.rows - w.group * rows);
+    rec[kRPieces] = w.more;
+}
+
+// ------------------------------------------------------------- many rows ---
+template <int D, int BITS, typename T>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2)
+mx_wide_kernel(MxArgs a, PackView pv) {
+    constexpr int EL = D / 8;             // elements of a thread's run: 8 threads to a key
+    constexpr int CB = EL * BITS / 8;     // their code bytes: 2, 4, 8 or 16
+    constexpr int CW = (CB + 3) / 4;
+    __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][kTile * D];   // stage, K and V
+    __shared__ int nan_tile[2];
+    using R = Rows<D, T>;
+    constexpr int KK = R::KK, DT = R::DT, NP = R::NP;
+
+    Walk<kWideRows> walk;
+    if (!walk.begin(a, pv)) return;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int my_key = tid >> 3, my_run = tid & 7;
+    const int slot_mask = (1 << a.ps_shift) - 1;
+    int made = 0;             // pieces of a unit that this share begins and does not end
+    Piece w;
+    while (walk.next(a, pv, w)) {
+        const Req r = walk.r;
+        const int32_t* pt = a.page_table + (size_t)r.b * a.max_pages;
+        const int r_local = wave * 32 + n, row = w.group * kWideRows + r_local;
+        const bool row_ok = row < r.rows;
+        const bool wave_ok =
+            __builtin_amdgcn_readfirstlane(w.group * kWideRows + wave * 32) < r.rows;
+        const int ga = a.g * a.bl;
+        const int last_row = min((w.group + 1) * kWideRows, r.rows) - 1;
+        const int ke = r.o + (last_row / ga + 1) * a.bl;                 // keys of the unit
+        const int all = r.o + (w.group * kWideRows / ga + 1) * a.bl;     // that every row sees
+        R x;
+        x.clear();
+        x.seen = r.o + (min(row, last_row) / ga + 1) * a.bl;
+        const T* q = static_cast<const T*>(a.q) +
+                     ((size_t)(r.row0 + (row_ok ? row / a.g : 0)) * a.Hq + w.head * a.g +
+                      (row_ok ? row % a.g : 0)) * D;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) query8(q + kk * 16 + h * 8, row_ok, x.qf[kk]);
+
+        // a thread's run of a tile: key tid / 8, elements (tid % 8) EL ...
+        uint32_t kraw[CW], vraw[CW], ksc, vsc;
+        bool ok, page_err = false;
+        auto load_tile = [&](int t) {
+            const int pos = t * kTile + my_key;
+            ok = pos < ke;
+            const int p = min(pos, ke - 1);
+            int page = pt[p >> a.ps_shift];
+            if ((unsigned)page >= (unsigned)a.num_pages) {   // read as page 0
+                page_err = true;
+                page = 0;
+            }
+            const size_t slot = (((size_t)page * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
+            load_codes<CB>(a.kc + slot * (D * BITS / 8) + my_run * CB, kraw);
+            load_codes<CB>(a.vc + slot * (D * BITS / 8) + my_run * CB, vraw);
+            ksc = a.ks[slot * DT + my_run * EL / 32];
+            vsc = a.vs[slot * DT + my_run * EL / 32];
+        };
+        auto store_run = [&](uint16_t* tile, const uint32_t* raw, uint32_t sc, bool good) {
+            const float s = mx_scale(sc);
+            if constexpr (EL == 4) {
+                bf16x2 v[4];
+                if constexpr (BITS == 4) {
+                    v[0] = mx_pair<4, 0>(raw[0], s);
+                    v[1] = mx_pair<4, 1>(raw[0], s);
+                } else {
+                    mx_dword<8>(raw[0], s, v);
+                }
+                const u32x2 y = {good ? __builtin_bit_cast(uint32_t, v[0]) : 0u,
+                                 good ? __builtin_bit_cast(uint32_t, v[1]) : 0u};
+                *reinterpret_cast<u32x2*>(tile + swz<D>(my_key, my_run / 2) + my_run % 2 * 4) = y;
+            } else {
+#pragma unroll
+                for (int i = 0; i < EL / 8; ++i)
+                    *reinterpret_cast<u32x4*>(tile + swz<D>(my_key, my_run * (EL / 8) + i)) =
+                        eight_values<BITS>(raw + i * (BITS / 4), s, good);
+            }
+        };
+
+        load_tile(w.k0);
+        for (int t = w.k0; t < w.k1; ++t) {
+            const int st = t & 1;
+            const bool masked = (t + 1) * kTile > all;
+            // (every wave left this stage before the last barrier)
+            if (masked && tid == 0) nan_tile[st] = 0;
+            if (masked) __syncthreads();
+            const bool bad = masked && ok && vsc == 255;
+            if (bad) nan_tile[st] = 1;
+            store_run(lds[st][0], kraw, ksc, ok);
+            store_run(lds[st][1], vraw, vsc, ok && !bad);
+            if (t + 1 < w.k1) load_tile(t + 1);
+            __syncthreads();
+            if (!wave_ok) continue;
+            floatx16 s = floatx16{};
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds[st][0] + swz<D>(n, kk * 2 + h));
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, x.qf[kk][p], s, 0, 0, 0);
+            }
+            bf16x8 pb[2][NP];
+            x.softmax(s, a.scale_log2, x.seen - t * kTile, masked, pb);
+            x.add_values(lds[st][1], pb);
+            if (masked && nan_tile[st]) x.spoil(a, pt, w.head, t * kTile, ke);
+        }
+        if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
+        x.store(a, r, w, r_local, kWideRows);
+        if (w.more > 0) {
+            made = w.more;
+            if (tid == 0) store_record(a, walk.index, r, w, kWideRows);
+        }
+        __syncthreads();   // the next piece fills the stages
+    }
+    if (made == 0 && tid == 0) a.rec[(size_t)walk.index * kRecInts + kRPieces] = 0;
+}
+
+// -------------------------------------------------------------- few rows ---
+// What the lanes of a wave wrote to LDS is there for all of them.
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <int D, int BITS, typename T>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2)
+mx_few_kernel(MxArgs a, PackView pv) {
+    constexpr int CB = D / 2 * BITS / 8;   // code bytes of half a key: a lane's
+    constexpr int CW = CB / 4;
+    constexpr int SC = D >= 64 ? D / 64 : 1;
+    using R = Rows<D, T>;
+    constexpr int KK = R::KK, DT = R::DT, NP = R::NP;
+    // each wave's V tile; at a piece's end the results of two waves
+    constexpr int kJoin = DT * 16 * 64 * 2;   // floats
+    union Lds {
+        uint16_t v[4][kTile * D];
+        float join[kJoin];
+    };
+    __shared__ __attribute__((aligned(16))) Lds lds;
+    __shared__ float stat[2][2][64];
+
+    Walk<kFewRows> walk;
+    if (!walk.begin(a, pv)) return;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int slot_mask = (1 << a.ps_shift) - 1;
+    uint16_t* vt = lds.v[wave];
+    int made = 0;
+    Piece w;
+    while (walk.next(a, pv, w)) {
+        const Req r = walk.r;
+        const int32_t* pt = a.page_table + (size_t)r.b * a.max_pages;
+        const int row = w.group * kFewRows + n;
+        const bool row_ok = row < r.rows;
+        const int ga = a.g * a.bl;
+        const int last_row = min((w.group + 1) * kFewRows, r.rows) - 1;
+        const int ke = r.o + (last_row / ga + 1) * a.bl;
+        const int all = r.o + (w.group * kFewRows / ga + 1) * a.bl;
+        R x;
+        x.clear();
+        x.seen = r.o + (min(row, last_row) / ga + 1) * a.bl;
+        // lane half h takes channels h D/2 ..; eight of them go to each product
+        const T* q = static_cast<const T*>(a.q) +
+                     ((size_t)(r.row0 + (row_ok ? row / a.g : 0)) * a.Hq + w.head * a.g +
+                      (row_ok ? row % a.g : 0)) * D + h * (D / 2);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) query8(q + kk * 8, row_ok, x.qf[kk]);
+
+        uint32_t kraw[CW], vraw[CW];
+        uint8_t ksc[SC], vsc[SC];
+        bool ok, page_err = false;
+        auto load_tile = [&](int t) {
+            const int pos = t * kTile + n;
+            ok = pos < ke;
+            const int p = min(pos, ke - 1);
+            int page = pt[p >> a.ps_shift];
+            if ((unsigned)page >= (unsigned)a.num_pages) {   // read as page 0
+                page_err = true;
+                page = 0;
+            }
+            const size_t slot = (((size_t)page * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
+            load_codes<CB>(a.kc + slot * (D * BITS / 8) + h * CB, kraw);
+            load_codes<CB>(a.vc + slot * (D * BITS / 8) + h * CB, vraw);
+#pragma unroll
+            for (int i = 0; i < SC; ++i) {
+                ksc[i] = a.ks[slot * DT + (D >= 64 ? h * SC : 0) + i];
+                vsc[i] = a.vs[slot * DT + (D >= 64 ? h * SC : 0) + i];
+            }
+        };
+        if (w.k0 + wave < w.k1) load_tile(w.k0 + wave);
+        for (int t = w.k0 + wave; t < w.k1; t += 4) {
+            const bool masked = (t + 1) * kTile > all;
+            floatx16 s = floatx16{};
+            bool bad[SC];
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                constexpr int PG = D >= 64 ? 4 : KK;      // pieces of eight to a group
+                const u32x4 kf =
+                    eight_values<BITS>(kraw + kk * (BITS / 4), mx_scale(ksc[kk / PG]), ok);
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                                x.qf[kk][p], s, 0, 0, 0);
+                bad[kk / PG] = masked && ok && vsc[kk / PG] == 255;
+                *reinterpret_cast<u32x4*>(vt + swz<D>(n, h * KK + kk)) =
+                    eight_values<BITS>(vraw + kk * (BITS / 4), mx_scale(vsc[kk / PG]),
+                                       ok && !bad[kk / PG]);
+            }
+            bool any_bad = false;
+#pragma unroll
+            for (int i = 0; i < SC; ++i) any_bad |= bad[i];
+            any_bad = __any(any_bad);
+            if (t + 4 < w.k1) load_tile(t + 4);
+            wave_sync();
+            bf16x8 pb[2][NP];
+            x.softmax(s, a.scale_log2, x.seen - t * kTile, masked, pb);
+            x.add_values(vt, pb);
+            if (any_bad) x.spoil(a, pt, w.head, t * kTile, ke);
+            wave_sync();   // the next tile's values go to the same place
+        }
+        if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
+
+        // waves 2 and 3 join 0 and 1, then 1 joins 0
+#pragma unroll
+        for (int from = 2; from >= 1; from >>= 1) {
+            __syncthreads();
+            const bool gives = wave >= from && wave < 2 * from;
+            const int to = wave & (from - 1);
+            float* j = lds.join + to * (kJoin / 2);
+            if (gives) {
+                stat[to][0][lane] = x.thr == -INFINITY ? -INFINITY : x.m_sub;
+                stat[to][1][lane] = x.l;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) j[(dt * 16 + i) * 64 + lane] = x.o[dt][i];
+            }
+            __syncthreads();
+            if (wave < from) {
+                // (a side without a score above -inf has no weight, but its NaN counts)
+                const float m0 = x.thr == -INFINITY ? -INFINITY : x.m_sub, m1 = stat[to][0][lane];
+                const float m = fmaxf(m0, m1);
+                const float f0 = m0 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m0 - m);
+                const float f1 = m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m1 - m);
+                if (m > -INFINITY) {
+                    x.m_sub = m;
+                    x.thr = m;
+                }
+                x.l = x.l * f0 + stat[to][1][lane] * f1;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        x.o[dt][i] = x.o[dt][i] * f0 + j[(dt * 16 + i) * 64 + lane] * f1;
+            }
+        }
+        if (wave == 0) x.store(a, r, w, n, kFewRows);
+        if (w.more > 0) {
+            made = w.more;
+            if (tid == 0) store_record(a, walk.index, r, w, kFewRows);
+        }
+        __syncthreads();
+    }
+    if (made == 0 && tid == 0) a.rec[(size_t)walk.index * kRecInts + kRPieces] = 0;
+}
+
+// ---------------------------------------------------------------- merge ---
+// A workgroup merges R rows of a divided unit: the unit's first piece in slot
+// 2 i + 1 of the share i that it began in, the others in slots 2 (i + 1), 2 (i
+// + 2), ...  256 / (D / 4) threads to a channel quad: R rows, and PL lanes that
+// take the pieces in turn.
+template <int D, typename T, int R>
+__global__ void __launch_bounds__(kThreads)
+mx_merge_kernel(MxArgs a, int rows) {
+    constexpr int Q = D / 4, PL = kThreads / Q / R;
+    __shared__ float m_of[PL][R], den_of[PL][R];
+    __shared__ float4 acc_of[PL][R][Q];
+    const int parts = rows / R;
+    const int i = blockIdx.x / parts, part = blockIdx.x % parts;
+    if (i >= a.head[0]) return;
+    const int32_t* rec = a.rec + (size_t)i * kRecInts;
+    const int pieces = rec[kRPieces];
+    const int row0 = rec[kRRow0], head = rec[kRHead], first = rec[kRFirst], n = rec[kRRows];
+    if (pieces == 0 || part * R >= n) return;
+    const int d4 = threadIdx.x % Q, rl = threadIdx.x / Q % R, pl = threadIdx.x / Q / R;
+    const int r = min(part * R + rl, n - 1);
+    auto slot = [&](int k) {
+        return (size_t)(k == 0 ? 2 * i + 1 : 2 * (i + k)) * rows + r;
+    };
+    float m = -INFINITY, den = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int F = 4;   // pieces in flight
+    for (int k0 = pl; k0 < pieces; k0 += F * PL) {
+        float lse[F];
+        float4 v[F];
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+            const size_t s = slot(min(k0 + j * PL, pieces - 1));
+            lse[j] = a.part_lse[s];
+            v[j] = *reinterpret_cast<const float4*>(a.part_o + s * D + d4 * 4);
+        }
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+            if (k0 + j * PL >= pieces || lse[j] == -INFINITY) continue;
+            const float m_new = fmaxf(m, lse[j]);
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+            const float x = __builtin_amdgcn_exp2f(lse[j] - m_new);
+            den = den * f + x;
+            acc.x = acc.x * f + x * v[j].x;
+            acc.y = acc.y * f + x * v[j].y;
+            acc.z = acc.z * f + x * v[j].z;
+            acc.w = acc.w * f + x * v[j].w;
+            m = m_new;
+        }
+    }
+    if constexpr (PL > 1) {
+        if (d4 == 0) m_of[pl][rl] = m, den_of[pl][rl] = den;
+        acc_of[pl][rl][d4] = acc;
+        __syncthreads();
+        if (pl > 0) return;
+#pragma unroll
+        for (int p = 1; p < PL; ++p) {
+            const float mp = m_of[p][rl];
+            const float4 v = acc_of[p][rl][d4];
+            if (mp == -INFINITY && den_of[p][rl] == 0.f) continue;
+            const float m_new = fmaxf(m, mp);
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+            const float x = __builtin_amdgcn_exp2f(mp - m_new);
+            den = den * f + den_of[p][rl] * x;
+            acc.x = acc.x * f + x * v.x;
+            acc.y = acc.y * f + x * v.y;
+            acc.z = acc.z * f + x * v.z;
+            acc.w = acc.w * f + x * v.w;
+            m = m_new;
+        }
+    }
+    if (part * R + rl >= n) return;
+    const float id = 1.0f / den;
+    const int row = first + r;
+    T* dst = static_cast<T*>(a.out) +
+             ((size_t)(row0 + row / a.g) * a.Hq + head * a.g + row % a.g) * D + d4 * 4;
+    store4(dst, acc.x * id, acc.y * id, acc.z * id, acc.w * id);
+}
+
+}  // namespace
+
+MxAttnSizes mx_attention_sizes(const fb_pack* pack, const fb_attn_shape* sh, int cu_count) {
+    MxAttnSizes z{};
+    const long long most = (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv);
+    z.rows = most <= kFewRows ? kFewRows : kWideRows;
+    const int per_cu = sh->dtype == FB_BF16 ? 3 : 2;   // as many as a CU holds at once
+    z.wgs = (per_cu * (cu_count > 0 ? cu_count : 256) + 7) / 8 * 8;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off += (bytes + 255) & ~(size_t)255;
+        return at;
+    };
+    z.off_head = take(16);
+    z.off_rec = take((size_t)z.wgs * kRecInts * sizeof(int32_t));
+    z.off_o = take((size_t)2 * z.wgs * z.rows * sh->head_dim * sizeof(float));
+    z.off_lse = take((size_t)2 * z.wgs * z.rows * sizeof(float));
+    z.total = off;
+    return z;
+}
+
+hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const int32_t* page_table,
+                               const fb_pack* pack, const fb_attn_shape* sh, void* out, void* wsp,
+                               const MxAttnSizes& z, hipStream_t stream) {
+    const float scale = sh->sm_scale > 0.f ? sh->sm_scale : 1.0f / sqrtf((float)sh->head_dim);
+    char* ws = static_cast<char*>(wsp);
+    const MxArgs a{q,
+                   static_cast<const uint8_t*>(cache->k_codes),
+                   static_cast<const uint8_t*>(cache->k_scales),
+                   static_cast<const uint8_t*>(cache->v_codes),
+                   static_cast<const uint8_t*>(cache->v_scales),
+                   page_table,
+                   out,
+                   reinterpret_cast<int32_t*>(ws + z.off_head),
+                   reinterpret_cast<int32_t*>(ws + z.off_rec),
+                   reinterpret_cast<float*>(ws + z.off_o),
+                   reinterpret_cast<float*>(ws + z.off_lse),
+                   sh->Hq, sh->Hkv, sh->Hq / sh->Hkv, pack->bl, pack->B, pack->W_max,
+                   pack->row_cap, z.wgs, log2_of(sh->page_size), sh->max_pages, sh->num_pages,
+                   scale * kLog2e};
+    auto launch = [&](auto d_c, auto bits_c, auto zero) {
+        constexpr int D = decltype(d_c)::value, BITS = decltype(bits_c)::value;
+        using T = decltype(zero);
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(z.wgs), dim3(kThreads), 0, stream, a, pack_view(pack));
+        };
+        auto merge = [&](auto kernel, int rows) {
+            hipLaunchKernelGGL(kernel, dim3(z.wgs * (z.rows / rows)), dim3(kThreads), 0, stream, a,
+                               z.rows);
+        };
+        if (z.rows == kFewRows) {
+            go(mx_few_kernel<D, BITS, T>);
+            merge(mx_merge_kernel<D, T, 1>, 1);
+        } else {
+            go(mx_wide_kernel<D, BITS, T>);
+            merge(mx_merge_kernel<D, T, 8>, 8);
+        }
+    };
+    auto of_type = [&](auto d_c, auto bits_c) {
+        if (sh->dtype == FB_BF16) launch(d_c, bits_c, uint16_t());
+        else launch(d_c, bits_c, float());
+    };
+    auto of_format = [&](auto d_c) {
+        if (cache->format == FB_MX4) of_type(d_c, std::integral_constant<int, 4>{});
+        else of_type(d_c, std::integral_constant<int, 8>{});
+    };
+    if (sh->head_dim == 32) of_format(std::integral_constant<int, 32>{});
+    else if (sh->head_dim == 64) of_format(std::integral_constant<int, 64>{});
+    else of_format(std::integral_constant<int, 128>{});
+    return hipGetLastError();
+}
+
+}  // namespace fb
