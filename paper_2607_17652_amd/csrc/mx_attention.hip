@@ -30,6 +30,7 @@
 // fp32: queries and weights are split into three bf16 parts, which hold all 24
 // bits, so there are three products each.
 #include <type_traits>
+#include <utility>
 
 #include "cache.h"
 
@@ -52,8 +53,6 @@ constexpr float kRescaleSlack = 8.0f;  // the running maximum may lag by 2^8
 
 struct MxArgs {
     const void* q;
-    const uint8_t *kc, *ks, *vc, *vs;
-    const int32_t* page_table;
     void* out;
     int32_t* head;     // [0]: workgroups with a share
     int32_t* rec;      // [wgs][8]: the unit whose first piece the workgroup made
@@ -62,9 +61,22 @@ struct MxArgs {
     int Hq, Hkv, g, bl, B, W_max, row_cap, wgs, ps_shift, max_pages, num_pages;
     float scale_log2;
 };
+// What a kernel only reads, apart from its other arguments, so that the compiler may
+// use scalar loads.
+#define MX_CACHE_PARAMS                                                                  \
+    const uint8_t *__restrict__ kc, const uint8_t *__restrict__ ks,                      \
+        const uint8_t *__restrict__ vc, const uint8_t *__restrict__ vs,                  \
+        const int32_t *__restrict__ page_table
 enum RecField { kRRow0 = 0, kRHead, kRFirst, kRRows, kRPieces, kRecInts = 8 };
 
 // ----------------------------------------------------------- the shares ---
+// The same value in every lane of the wave, said to the compiler.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline long long uniform(long long x) {
+    return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 |
+                       (uint32_t)uniform((int)x));
+}
+
 // A request's part of the line.
 struct Req {
     int b, row0, o, rows, groups;
@@ -141,6 +153,7 @@ struct Walk {
             if (i < wave) sum += wave_sum[i];
             total += wave_sum[i];
         }
+        total = uniform(total);
         share = max((total + a.wgs - 1) / a.wgs, (long long)(kLeastShare + kStart));
         const int busy = (int)((total + share - 1) / share);
         // Neighbours in the line read the same keys, so they belong on one XCD:
@@ -164,8 +177,8 @@ struct Walk {
             found[1] = before;
         }
         __syncthreads();
-        r = request<ROWS>(a, pv, (int)found[0], false);
-        at = found[1];
+        r = request<ROWS>(a, pv, uniform((int)found[0]), false);
+        at = uniform(found[1]);
         head = (int)((p - at) / r.len);
         at += (long long)head * r.len;
         group = 0;
@@ -248,17 +261,31 @@ __device__ inline void store4(float* p, float a, float b, float c, float d) {
     *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
 }
 
-// Where the 16-byte piece c of row r of a [32][D] bf16 tile lies in LDS, in
-// elements.  Free of bank conflicts are so: sixteen rows' same piece (key
-// operands; sixteen lanes a step); four neighbouring rows' same 64 bytes (value
-// operands, read transposed); two rows' alternate pieces (the stores of a tile
-// at D = 128, eight threads to a row).
+// Where the 16-byte piece c of row r of a 32-key tile lies in LDS, in elements.
+// Rows are padded where tiles are shared, so that the pieces of a row lie at fixed
+// distances: sixteen rows' same piece (key operands; a read goes sixteen lanes a
+// step) and four neighbouring rows' same 64 bytes (value operands, read transposed)
+// then lie in different banks.
 template <int D>
-__device__ inline int swz(int r, int c) {
-    if constexpr (D == 128) return r * D + ((c ^ ((r & 3) << 2 | (((r >> 2) & 3) ^ (r & 1)))) * 8);
-    else if constexpr (D == 64) return r * D + ((c ^ (((r >> 1) & 1) << 2 | ((r >> 2) & 3))) * 8);
-    else return r * D + ((c ^ ((r >> 2) & 3)) * 8);
-}
+struct KeyRows {
+    static constexpr int kPitch = D + 8;
+    __device__ static inline int at(int r, int c) { return r * kPitch + c * 8; }
+};
+template <int D>
+struct ValueRows {
+    static constexpr int kPitch = D == 32 ? 32 : D + 32;
+    __device__ static inline int at(int r, int c) { return r * kPitch + c * 8; }
+};
+// A wave's own values are stored by sixteen rows' same piece too, for which no
+// padding serves both: pieces change places by their row's number instead.
+template <int D>
+struct TurnedRows {
+    __device__ static inline int at(int r, int c) {
+        const int turn = D == 128 ? (r & 3) << 2 | ((r >> 2) & 3)
+                       : D == 64 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r >> 2) & 3;
+        return r * D + (c ^ turn) * 8;
+    }
+};
 
 // Values of column l % 16 and four neighbouring rows: lane i of each sixteen
 // gives the address of row i / 4, columns 4 (i % 4) ...
@@ -271,25 +298,31 @@ __device__ inline s16x4 read_tr(const uint16_t* p) {
 __device__ inline float half_max(float x) {
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
                                                      false);
-    return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    float r;   // (plain v_max: the compiler would first make both sides canonical)
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(__uint_as_float(sw[0])), "v"(__uint_as_float(sw[1])));
+    return r;
 }
+
+typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
 
 // N bytes of codes as dwords.
 template <int N>
-__device__ inline void load_codes(const uint8_t* p, uint32_t* q) {
-    if constexpr (N == 2) q[0] = *reinterpret_cast<const uint16_t*>(p);
-    else if constexpr (N == 4) q[0] = *reinterpret_cast<const uint32_t*>(p);
+__device__ inline void load_codes(GlobalBytes p, uint32_t* q) {
+#define MX_AT(type, at) (*(const __attribute__((address_space(1))) type*)(p + (at)))
+    if constexpr (N == 2) q[0] = MX_AT(uint16_t, 0);
+    else if constexpr (N == 4) q[0] = MX_AT(uint32_t, 0);
     else if constexpr (N == 8) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        const u32x2 x = MX_AT(u32x2, 0);
         q[0] = x[0], q[1] = x[1];
     } else {
 #pragma unroll
         for (int j = 0; j < N / 16; ++j) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(p + 16 * j);
+            const u32x4 x = MX_AT(u32x4, 16 * j);
 #pragma unroll
             for (int i = 0; i < 4; ++i) q[4 * j + i] = x[i];
         }
     }
+#undef MX_AT
 }
 
 // Eight values from their codes (BITS / 4 dwords), zeros unless ok.
@@ -322,19 +355,17 @@ struct Rows {
         thr = -INFINITY;
     }
 
-    // Scores into P^T and the running statistics; keys from `left` on (of the
-    // lane's row) are not seen.
-    __device__ inline void softmax(floatx16& s, float scale, int left, bool masked,
-                                   bf16x8 (&pb)[2][NP]) {
+    // Keys from `left` on are not seen.
+    __device__ inline void mask(floatx16& s, int left) {
         const int h = (threadIdx.x >> 5) & 1;
-        if (masked)
 #pragma unroll
-            for (int x = 0; x < 16; ++x)
-                if (8 * (x >> 2) + 4 * h + (x & 3) >= left) s[x] = -INFINITY;
-        float mx = s[0];
-#pragma unroll
-        for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x]);
-        mx = half_max(mx);
+        for (int x = 0; x < 16; ++x)
+            if (8 * (x >> 2) + 4 * h + (x & 3) >= left) s[x] = -INFINITY;
+    }
+
+    // The running maximum moves when a tile's passes it by 2^8, so that results are
+    // seldom rescaled; weights are up to 2^8 then.
+    __device__ inline void rescale(float mx, float scale) {
         const bool need = mx > thr;
         if (__any(need)) {
             const float m_new = need ? mx * scale : m_sub;
@@ -348,60 +379,76 @@ struct Rows {
             m_sub = m_new;
             if (need) thr = mx + kRescaleSlack / scale;
         }
-        // bf16: the weights are rounded for the product, and the denominator sums
-        // the rounded ones, so that the rounding cancels where values agree
+    }
+
+    // Scores x0 .. x0 + N - 1 into weights.  bf16: they are rounded for the product,
+    // and the denominator sums the rounded ones, so that the rounding cancels where
+    // values agree.
+    template <int N>
+    __device__ inline void weights(const floatx16& s, int x0, float scale, bf16x8 (&pb)[2][NP]) {
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[x], scale, -m_sub));
+        for (int x = x0; x < x0 + N; x += 2) {
+            float p[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                p[i] = __builtin_amdgcn_exp2f(fmaf(s[x + i], scale, -m_sub));
             if constexpr (NP == 1) {
-                pb[x >> 3][0][x & 7] = (__bf16)p;
+                const bf16x2 pr = {(__bf16)p[0], (__bf16)p[1]};
+                const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+                pb[x >> 3][0][x & 7] = pr[0];
+                pb[x >> 3][0][(x & 7) + 1] = pr[1];
+                l = __builtin_amdgcn_fdot2_f32_bf16(pr, one, l, false);
             } else {
-                __bf16 part[3];
-                split3(p, part);
 #pragma unroll
-                for (int k = 0; k < 3; ++k) pb[x >> 3][k][x & 7] = part[k];
-                l += p;
-            }
-        }
-        if constexpr (NP == 1) {
-            const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+                for (int i = 0; i < 2; ++i) {
+                    __bf16 part[3];
+                    split3(p[i], part);
 #pragma unroll
-            for (int x = 0; x < 8; x += 2) {
-                l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[0][0][x], pb[0][0][x + 1]}, one, l, false);
-                l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[1][0][x], pb[1][0][x + 1]}, one, l, false);
+                    for (int k = 0; k < 3; ++k) pb[x >> 3][k][(x & 7) + i] = part[k];
+                    l += p[i];
+                }
             }
         }
     }
 
-    // O^T += V^T P^T with V the tile at vt.
-    __device__ inline void add_values(const uint16_t* vt, const bf16x8 (&pb)[2][NP]) {
+    // A whole tile's scores into weights, with the running statistics.
+    __device__ inline void softmax(floatx16& s, float scale, bf16x8 (&pb)[2][NP]) {
+        float mx = s[0];
+#pragma unroll
+        for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x]);
+        rescale(half_max(mx), scale);
+        weights<16>(s, 0, scale, pb);
+    }
+
+    // The operand V^T of keys 16 t .. 16 t + 15 and channels 32 dt ..: slots 8 h .. hold
+    // keys 16 t + 4 h .. + 3, then 16 t + 8 + 4 h .. + 3.
+    template <typename L>
+    __device__ static inline bf16x8 values(const uint16_t* vt, int t, int dt) {
         const int lane = threadIdx.x & 63, h = lane >> 5;
+        const int row = 16 * t + 4 * h + (lane & 15) / 4;
+        const int piece = dt * 4 + (lane & 16) / 8 + (lane & 3) / 2, in = (lane & 1) * 4;
+        union {
+            s16x4 part[2];
+            bf16x8 v;
+        } f;
+        f.part[0] = read_tr(vt + L::at(row, piece) + in);
+        f.part[1] = read_tr(vt + L::at(row + 8, piece) + in);
+        return f.v;
+    }
+    __device__ inline void add(const bf16x8& v, int dt, const bf16x8 (&p)[NP]) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                // slots 8 h ...: keys 16 t + 4 h .. + 3, then 16 t + 8 + 4 h .. + 3
-                const int row = 16 * t + 4 * h + (lane & 15) / 4;
-                const int piece = dt * 4 + (lane & 16) / 8 + (lane & 3) / 2, in = (lane & 1) * 4;
-                union {
-                    s16x4 part[2];
-                    bf16x8 v;
-                } f;
-                f.part[0] = read_tr(vt + swz<D>(row, piece) + in);
-                f.part[1] = read_tr(vt + swz<D>(row + 8, piece) + in);
-#pragma unroll
-                for (int k = 0; k < NP; ++k)
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pb[t][k], o[dt], 0, 0, 0);
-            }
+        for (int k = 0; k < NP; ++k)
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k], o[dt], 0, 0, 0);
     }
 
     // Values of NaN scales in a tile that not every row sees were staged as zeros:
     // the rows that do see them get their NaN here.
-    __device__ inline void spoil(const MxArgs& a, const int32_t* pt, int head, int key0, int end) {
+    __device__ inline void spoil(const MxArgs& a, const uint8_t* vs, const int32_t* pt, int head, int key0,
+                                 int end) {
         for (int key = key0; key < min(key0 + kTile, end); ++key) {
             const int page = pt[key >> a.ps_shift];
             if ((unsigned)page >= (unsigned)a.num_pages) continue;
-            const uint8_t* s = a.vs + ((((size_t)page * a.Hkv + head) << a.ps_shift) +
+            const uint8_t* s = vs + ((((size_t)page * a.Hkv + head) << a.ps_shift) +
                                        (key & ((1 << a.ps_shift) - 1))) * DT;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
@@ -449,63 +496,99 @@ __device__ inline void store_record(const MxArgs& a, int index, const Req& r, co
 }
 
 // ------------------------------------------------------------- many rows ---
-template <int D, int BITS, typename T>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2)
-mx_wide_kernel(MxArgs a, PackView pv) {
+template <int N, typename F, int... I>
+__device__ __attribute__((always_inline)) inline void static_for_impl(F& f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+// f(std::integral_constant<int, 0>) ... f(std::integral_constant<int, N-1>)
+template <int N, typename F>
+__device__ __attribute__((always_inline)) inline void static_for(F&& f) {
+    static_for_impl<N>(f, std::make_integer_sequence<int, N>{});
+}
+
+// A step takes the scores of tile t + 1 on the matrix cores while the vector units
+// turn those of tile t into weights, then adds tile t's values while it looks for
+// the next scores' maximum and turns the codes of K(t + 2) and V(t + 1), loaded a
+// step before, into bf16.  Two stages of K and of V are enough then, and one
+// barrier a step.
+// PAGED: a page holds whole tiles, so a tile's loads share one scalar base.
+// FULL: every wave of a unit has query rows.
+template <int D, int BITS, typename T, bool PAGED, bool FULL>
+__global__ void __launch_bounds__(kThreads, 2)
+mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     constexpr int EL = D / 8;             // elements of a thread's run: 8 threads to a key
     constexpr int CB = EL * BITS / 8;     // their code bytes: 2, 4, 8 or 16
     constexpr int CW = (CB + 3) / 4;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][kTile * D];   // stage, K and V
-    __shared__ int nan_tile[2];
-    using R = Rows<D, T>;
-    constexpr int KK = R::KK, DT = R::DT, NP = R::NP;
+    constexpr int KK = D / 16, DT = D / 32, NP = kParts<T>;
+    constexpr int kRowBytes = D * BITS / 8;
+    using KR = KeyRows<D>;
+    using VR = ValueRows<D>;
+    __shared__ __attribute__((aligned(16))) uint16_t lds_k[2][kTile * KR::kPitch];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_v[2][kTile * VR::kPitch];
 
     Walk<kWideRows> walk;
     if (!walk.begin(a, pv)) return;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int my_key = tid >> 3, my_run = tid & 7;
     const int slot_mask = (1 << a.ps_shift) - 1;
-    int made = 0;             // pieces of a unit that this share begins and does not end
+    const uint32_t code_at = my_key * kRowBytes + my_run * CB;
+    const uint32_t scale_at = my_key * DT + my_run * EL / 32;
+    const int k_at = KR::at(n, h);        // a key operand's piece 2 kk + h lies 16 kk on
+    bool made = false;        // a unit that this share begins and does not end
     Piece w;
     while (walk.next(a, pv, w)) {
         const Req r = walk.r;
-        const int32_t* pt = a.page_table + (size_t)r.b * a.max_pages;
+        const int32_t* pt = page_table + (size_t)r.b * a.max_pages;
         const int r_local = wave * 32 + n, row = w.group * kWideRows + r_local;
-        const bool row_ok = row < r.rows;
-        const bool wave_ok =
-            __builtin_amdgcn_readfirstlane(w.group * kWideRows + wave * 32) < r.rows;
+        const bool row_ok = FULL || row < r.rows;
+        const bool wave_ok = FULL || uniform(w.group * kWideRows + wave * 32) < r.rows;
         const int ga = a.g * a.bl;
         const int last_row = min((w.group + 1) * kWideRows, r.rows) - 1;
         const int ke = r.o + (last_row / ga + 1) * a.bl;                 // keys of the unit
         const int all = r.o + (w.group * kWideRows / ga + 1) * a.bl;     // that every row sees
-        R x;
+        Rows<D, T> x;
         x.clear();
         x.seen = r.o + (min(row, last_row) / ga + 1) * a.bl;
-        const T* q = static_cast<const T*>(a.q) +
-                     ((size_t)(r.row0 + (row_ok ? row / a.g : 0)) * a.Hq + w.head * a.g +
-                      (row_ok ? row % a.g : 0)) * D;
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) query8(q + kk * 16 + h * 8, row_ok, x.qf[kk]);
 
         // a thread's run of a tile: key tid / 8, elements (tid % 8) EL ...
         uint32_t kraw[CW], vraw[CW], ksc, vsc;
-        bool ok, page_err = false;
-        auto load_tile = [&](int t) {
-            const int pos = t * kTile + my_key;
-            ok = pos < ke;
-            const int p = min(pos, ke - 1);
-            int page = pt[p >> a.ps_shift];
-            if ((unsigned)page >= (unsigned)a.num_pages) {   // read as page 0
-                page_err = true;
-                page = 0;
+        bool page_err = false, bad = false;
+        auto page_of = [&](int t) { return pt[(t * kTile) >> a.ps_shift]; };   // PAGED
+        // The place of tile t among the cache's slots: of its first key (PAGED, `page` its
+        // page), of this thread's key else.  A bad page id is read as page 0.
+        auto place = [&](int t, int page) -> size_t {
+            int p = t * kTile;
+            if constexpr (!PAGED) {
+                p = min(p + my_key, ke - 1);
+                page = pt[p >> a.ps_shift];
             }
-            const size_t slot = (((size_t)page * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
-            load_codes<CB>(a.kc + slot * (D * BITS / 8) + my_run * CB, kraw);
-            load_codes<CB>(a.vc + slot * (D * BITS / 8) + my_run * CB, vraw);
-            ksc = a.ks[slot * DT + my_run * EL / 32];
-            vsc = a.vs[slot * DT + my_run * EL / 32];
+            const bool good = (unsigned)page < (unsigned)a.num_pages;
+            page_err |= !good;
+            return (((size_t)(good ? page : 0) * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
         };
-        auto store_run = [&](uint16_t* tile, const uint32_t* raw, uint32_t sc, bool good) {
+        auto load_run = [&](const uint8_t* codes, const uint8_t* scales, size_t slot, uint32_t* raw,
+                            uint32_t& sc) {
+            if constexpr (PAGED) {
+                // (scalar bases and a lane's 32-bit offsets: the compiler would keep the
+                // sums of a base and the offset, 64 bits a lane)
+                GlobalBytes c0 = (GlobalBytes)(codes + slot * kRowBytes);
+                GlobalBytes s0 = (GlobalBytes)(scales + slot * DT);
+                asm("" : "+s"(c0), "+s"(s0));
+                load_codes<CB>(c0 + code_at, raw);
+                sc = s0[scale_at];
+            } else {
+                load_codes<CB>((GlobalBytes)(codes + slot * kRowBytes + my_run * CB), raw);
+                sc = scales[slot * DT + my_run * EL / 32];
+            }
+        };
+        auto load_k = [&](size_t slot) { load_run(kc, ks, slot, kraw, ksc); };
+        auto load_v = [&](size_t slot) { load_run(vc, vs, slot, vraw, vsc); };
+        // Codes into a stage.  Keys past the unit's last one have no weight, not even
+        // as NaN, and neither has a NaN value for the rows that do not see it: both
+        // become zeros (the NaN is given to those that do see it at the end).
+        constexpr int NPC = EL < 8 ? 1 : EL / 8;      // pieces of a run
+        auto store_piece = [&](auto rows_c, uint16_t* tile, const uint32_t* raw, uint32_t sc, int i) {
+            using L = decltype(rows_c);
             const float s = mx_scale(sc);
             if constexpr (EL == 4) {
                 bf16x2 v[4];
@@ -515,53 +598,191 @@ mx_wide_kernel(MxArgs a, PackView pv) {
                 } else {
                     mx_dword<8>(raw[0], s, v);
                 }
-                const u32x2 y = {good ? __builtin_bit_cast(uint32_t, v[0]) : 0u,
-                                 good ? __builtin_bit_cast(uint32_t, v[1]) : 0u};
-                *reinterpret_cast<u32x2*>(tile + swz<D>(my_key, my_run / 2) + my_run % 2 * 4) = y;
+                *reinterpret_cast<u32x2*>(tile + L::at(my_key, my_run / 2) + my_run % 2 * 4) =
+                    u32x2{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1])};
             } else {
-#pragma unroll
-                for (int i = 0; i < EL / 8; ++i)
-                    *reinterpret_cast<u32x4*>(tile + swz<D>(my_key, my_run * (EL / 8) + i)) =
-                        eight_values<BITS>(raw + i * (BITS / 4), s, good);
+                *reinterpret_cast<u32x4*>(tile + L::at(my_key, my_run * NPC + i)) =
+                    eight_values<BITS>(raw + i * (BITS / 4), s, true);
             }
         };
-
-        load_tile(w.k0);
-        for (int t = w.k0; t < w.k1; ++t) {
-            const int st = t & 1;
-            const bool masked = (t + 1) * kTile > all;
-            // (every wave left this stage before the last barrier)
-            if (masked && tid == 0) nan_tile[st] = 0;
-            if (masked) __syncthreads();
-            const bool bad = masked && ok && vsc == 255;
-            if (bad) nan_tile[st] = 1;
-            store_run(lds[st][0], kraw, ksc, ok);
-            store_run(lds[st][1], vraw, vsc, ok && !bad);
-            if (t + 1 < w.k1) load_tile(t + 1);
-            __syncthreads();
-            if (!wave_ok) continue;
-            floatx16 s = floatx16{};
+        auto store_run = [&](auto rows_c, uint16_t* tile, const uint32_t* raw, uint32_t sc) {
+#pragma unroll
+            for (int i = 0; i < NPC; ++i) store_piece(rows_c, tile, raw, sc, i);
+        };
+        auto zero_tail = [&](int t, uint32_t* raw, uint32_t& sc, bool value) {
+            if ((t + 1) * kTile <= all) return;
+            const bool past = t * kTile + my_key >= ke;
+            const bool nan = value && sc == 255;
+            bad |= nan && !past;
+            if (past || nan) {
+                sc = 127;
+#pragma unroll
+                for (int i = 0; i < CW; ++i) raw[i] = 0;
+            }
+        };
+        // (tile u of the piece is tile k0 + u of the unit and lies in stage u % 2)
+        const int k0 = w.k0, nt = w.k1 - w.k0;
+        // page ids, asked for a step before the tile's codes are
+        int pg1 = PAGED ? page_of(k0 + min(1, nt - 1)) : 0, pg2 = PAGED ? page_of(k0 + min(2, nt - 1)) : 0;
+        int pg_next = PAGED ? page_of(k0 + min(3, nt - 1)) : 0;
+        size_t slot = place(k0, PAGED ? page_of(k0) : 0);   // of the next values to be loaded
+        load_k(slot);
+        load_v(slot);
+        const T* q = static_cast<const T*>(a.q) +
+                     ((size_t)(r.row0 + (row_ok ? row / a.g : 0)) * a.Hq + w.head * a.g +
+                      (row_ok ? row % a.g : 0)) * D;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) query8(q + kk * 16 + h * 8, row_ok, x.qf[kk]);
+        zero_tail(k0, kraw, ksc, false);
+        store_run(KR{}, lds_k[0], kraw, ksc);
+        if (nt > 1) {
+            slot = place(k0 + 1, pg1);
+            load_k(slot);
+        }
+        __syncthreads();
+        floatx16 s_cur = floatx16{};
+        float mx = -INFINITY;
+        if (wave_ok) {
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds[st][0] + swz<D>(n, kk * 2 + h));
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds_k[0] + k_at + 16 * kk);
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, x.qf[kk][p], s, 0, 0, 0);
+                    s_cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, x.qf[kk][p], s_cur, 0, 0, 0);
             }
-            bf16x8 pb[2][NP];
-            x.softmax(s, a.scale_log2, x.seen - t * kTile, masked, pb);
-            x.add_values(lds[st][1], pb);
-            if (masked && nan_tile[st]) x.spoil(a, pt, w.head, t * kTile, ke);
+            if ((k0 + 1) * kTile > all) x.mask(s_cur, x.seen - k0 * kTile);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s_cur[i]);
+            mx = half_max(mx);
+            x.rescale(mx, a.scale_log2);
         }
+        zero_tail(k0, vraw, vsc, true);
+        store_run(VR{}, lds_v[0], vraw, vsc);
+        if (nt > 1) {
+            zero_tail(k0 + 1, kraw, ksc, false);
+            store_run(KR{}, lds_k[1], kraw, ksc);
+            load_v(slot);
+        }
+        if (nt > 2) {
+            slot = place(k0 + 2, pg2);
+            load_k(slot);
+        }
+        // KIND 0: a step whose loads all have tiles, which every row sees; 1: one near
+        // the end; 2: the last one
+        auto step = [&](int u, auto st_c, auto kind_c) __attribute__((always_inline)) {
+            constexpr int ST = decltype(st_c)::value;
+            constexpr int KIND = decltype(kind_c)::value;
+            constexpr bool LAST = KIND == 2, NEAR = KIND != 0;
+            const int t = k0 + u;
+            __syncthreads();
+            floatx16 s_nxt = floatx16{};
+            bf16x8 pb[2][NP];
+            if (wave_ok) {
+                constexpr int SPG = 16 / KK;
+                if constexpr (!LAST) {
+                    const uint16_t* kt = lds_k[1 - ST];
+                    bf16x8 fr[2];
+                    fr[0] = *reinterpret_cast<const bf16x8*>(kt + k_at);
+                    fr[1] = *reinterpret_cast<const bf16x8*>(kt + k_at + 16);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk) {
+                        const bf16x8 kf = fr[kk & 1];
+                        if (kk + 2 < KK)
+                            fr[kk & 1] = *reinterpret_cast<const bf16x8*>(kt + k_at + 16 * (kk + 2));
+#pragma unroll
+                        for (int p = 0; p < NP; ++p)
+                            s_nxt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, x.qf[kk][p], s_nxt,
+                                                                            0, 0, 0);
+                        x.template weights<SPG>(s_cur, kk * SPG, a.scale_log2, pb);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if (NEAR && (t + 2) * kTile > all) x.mask(s_nxt, x.seen - (t + 1) * kTile);
+                } else {
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk)
+                        x.template weights<SPG>(s_cur, kk * SPG, a.scale_log2, pb);
+                }
+            }
+            // The codes loaded a step ago go to LDS between the products; then the next
+            // tiles' are asked for.
+            const bool more_k = !LAST && (!NEAR || u + 2 < nt);
+            if constexpr (NEAR && !LAST) {
+                zero_tail(t + 1, vraw, vsc, true);
+                if (more_k) zero_tail(t + 2, kraw, ksc, false);
+            }
+            auto stage = [&](int i) __attribute__((always_inline)) {   // i < 2 NPC
+                if constexpr (!LAST) {
+                    if (i < NPC) store_piece(VR{}, lds_v[1 - ST], vraw, vsc, i);
+                    else if (more_k) store_piece(KR{}, lds_k[ST], kraw, ksc, i - NPC);
+                }
+            };
+            if (wave_ok) {
+                constexpr int NX = DT * 2, VPG = 16 / NX, EVERY = NX / (2 * NPC);
+                const uint16_t* vt = lds_v[ST];
+                bf16x8 fr[2];
+                fr[0] = Rows<D, T>::template values<VR>(vt, 0, 0);
+                fr[1] = Rows<D, T>::template values<VR>(vt, 1 / DT, 1 % DT);
+                mx = -INFINITY;
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < NX; ++i) {
+                    const bf16x8 vf = fr[i & 1];
+                    if (i + 2 < NX)
+                        fr[i & 1] = Rows<D, T>::template values<VR>(vt, (i + 2) / DT, (i + 2) % DT);
+                    x.add(vf, i % DT, pb[i / DT]);
+                    if constexpr (!LAST) {
+#pragma unroll
+                        for (int y = 0; y < VPG; ++y) mx = fmaxf(mx, s_nxt[i * VPG + y]);
+                        if (i % EVERY == 0) stage(i / EVERY);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2 * NPC; ++i) stage(i);
+            }
+            if constexpr (!LAST) {
+                if (more_k) load_v(slot);
+                if (!NEAR || u + 3 < nt) {
+                    slot = place(t + 3, pg_next);
+                    load_k(slot);
+                }
+                if constexpr (PAGED) pg_next = page_of(k0 + min(u + 4, nt - 1));
+                if (!wave_ok) return;
+                mx = half_max(mx);
+                x.rescale(mx, a.scale_log2);
+                s_cur = s_nxt;
+            }
+        };
+        using C0 = std::integral_constant<int, 0>;
+        using C1 = std::integral_constant<int, 1>;
+        using C2 = std::integral_constant<int, 2>;
+        // steps whose tile u + 3 is there and whose tile u + 2 every row sees
+        const int full = min(nt - 3, all / kTile - k0 - 2);
+        int u = 0;
+        for (; u + 2 <= full; u += 2) {
+            step(u, C0{}, C0{});
+            step(u + 1, C1{}, C0{});
+        }
+        for (; u + 1 < nt; ++u) {
+            if (u & 1) step(u, C1{}, C1{});
+            else step(u, C0{}, C1{});
+        }
+        if (u & 1) step(u, C1{}, C2{});
+        else step(u, C0{}, C2{});
         if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
+        // (the barrier also lets the next piece fill the stages)
+        if (__syncthreads_or(bad))
+            for (int t = all / kTile; t < w.k1; ++t)
+                if (t >= k0) x.spoil(a, vs, pt, w.head, t * kTile, ke);
         x.store(a, r, w, r_local, kWideRows);
         if (w.more > 0) {
-            made = w.more;
+            made = true;
             if (tid == 0) store_record(a, walk.index, r, w, kWideRows);
         }
-        __syncthreads();   // the next piece fills the stages
     }
-    if (made == 0 && tid == 0) a.rec[(size_t)walk.index * kRecInts + kRPieces] = 0;
+    if (!made && tid == 0) a.rec[(size_t)walk.index * kRecInts + kRPieces] = 0;
 }
 
 // -------------------------------------------------------------- few rows ---
@@ -572,8 +793,8 @@ __device__ inline void wave_sync() {
 }
 
 template <int D, int BITS, typename T>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2)
-mx_few_kernel(MxArgs a, PackView pv) {
+__global__ void __launch_bounds__(kThreads, 2)
+mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     constexpr int CB = D / 2 * BITS / 8;   // code bytes of half a key: a lane's
     constexpr int CW = CB / 4;
     constexpr int SC = D >= 64 ? D / 64 : 1;
@@ -593,11 +814,11 @@ mx_few_kernel(MxArgs a, PackView pv) {
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int slot_mask = (1 << a.ps_shift) - 1;
     uint16_t* vt = lds.v[wave];
-    int made = 0;
+    bool made = false;
     Piece w;
     while (walk.next(a, pv, w)) {
         const Req r = walk.r;
-        const int32_t* pt = a.page_table + (size_t)r.b * a.max_pages;
+        const int32_t* pt = page_table + (size_t)r.b * a.max_pages;
         const int row = w.group * kFewRows + n;
         const bool row_ok = row < r.rows;
         const int ga = a.g * a.bl;
@@ -627,12 +848,12 @@ mx_few_kernel(MxArgs a, PackView pv) {
                 page = 0;
             }
             const size_t slot = (((size_t)page * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
-            load_codes<CB>(a.kc + slot * (D * BITS / 8) + h * CB, kraw);
-            load_codes<CB>(a.vc + slot * (D * BITS / 8) + h * CB, vraw);
+            load_codes<CB>((GlobalBytes)(kc + slot * (D * BITS / 8) + h * CB), kraw);
+            load_codes<CB>((GlobalBytes)(vc + slot * (D * BITS / 8) + h * CB), vraw);
 #pragma unroll
             for (int i = 0; i < SC; ++i) {
-                ksc[i] = a.ks[slot * DT + (D >= 64 ? h * SC : 0) + i];
-                vsc[i] = a.vs[slot * DT + (D >= 64 ? h * SC : 0) + i];
+                ksc[i] = ks[slot * DT + (D >= 64 ? h * SC : 0) + i];
+                vsc[i] = vs[slot * DT + (D >= 64 ? h * SC : 0) + i];
             }
         };
         if (w.k0 + wave < w.k1) load_tile(w.k0 + wave);
@@ -650,7 +871,7 @@ mx_few_kernel(MxArgs a, PackView pv) {
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
                                                                 x.qf[kk][p], s, 0, 0, 0);
                 bad[kk / PG] = masked && ok && vsc[kk / PG] == 255;
-                *reinterpret_cast<u32x4*>(vt + swz<D>(n, h * KK + kk)) =
+                *reinterpret_cast<u32x4*>(vt + TurnedRows<D>::at(n, h * KK + kk)) =
                     eight_values<BITS>(vraw + kk * (BITS / 4), mx_scale(vsc[kk / PG]),
                                        ok && !bad[kk / PG]);
             }
@@ -661,9 +882,12 @@ mx_few_kernel(MxArgs a, PackView pv) {
             if (t + 4 < w.k1) load_tile(t + 4);
             wave_sync();
             bf16x8 pb[2][NP];
-            x.softmax(s, a.scale_log2, x.seen - t * kTile, masked, pb);
-            x.add_values(vt, pb);
-            if (any_bad) x.spoil(a, pt, w.head, t * kTile, ke);
+            if (masked) x.mask(s, x.seen - t * kTile);
+            x.softmax(s, a.scale_log2, pb);
+#pragma unroll
+            for (int i = 0; i < 2 * DT; ++i)
+                x.add(R::template values<TurnedRows<D>>(vt, i / DT, i % DT), i % DT, pb[i / DT]);
+            if (any_bad) x.spoil(a, vs, pt, w.head, t * kTile, ke);
             wave_sync();   // the next tile's values go to the same place
         }
         if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
@@ -704,12 +928,12 @@ mx_few_kernel(MxArgs a, PackView pv) {
         }
         if (wave == 0) x.store(a, r, w, n, kFewRows);
         if (w.more > 0) {
-            made = w.more;
+            made = true;
             if (tid == 0) store_record(a, walk.index, r, w, kFewRows);
         }
         __syncthreads();
     }
-    if (made == 0 && tid == 0) a.rec[(size_t)walk.index * kRecInts + kRPieces] = 0;
+    if (!made && tid == 0) a.rec[(size_t)walk.index * kRecInts + kRPieces] = 0;
 }
 
 // ---------------------------------------------------------------- merge ---
@@ -796,7 +1020,7 @@ MxAttnSizes mx_attention_sizes(const fb_pack* pack, const fb_attn_shape* sh, int
     MxAttnSizes z{};
     const long long most = (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv);
     z.rows = most <= kFewRows ? kFewRows : kWideRows;
-    const int per_cu = sh->dtype == FB_BF16 ? 3 : 2;   // as many as a CU holds at once
+    const int per_cu = 2;   // as many as a CU holds at once
     z.wgs = (per_cu * (cu_count > 0 ? cu_count : 256) + 7) / 8 * 8;
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -818,11 +1042,6 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
     const float scale = sh->sm_scale > 0.f ? sh->sm_scale : 1.0f / sqrtf((float)sh->head_dim);
     char* ws = static_cast<char*>(wsp);
     const MxArgs a{q,
-                   static_cast<const uint8_t*>(cache->k_codes),
-                   static_cast<const uint8_t*>(cache->k_scales),
-                   static_cast<const uint8_t*>(cache->v_codes),
-                   static_cast<const uint8_t*>(cache->v_scales),
-                   page_table,
                    out,
                    reinterpret_cast<int32_t*>(ws + z.off_head),
                    reinterpret_cast<int32_t*>(ws + z.off_rec),
@@ -835,7 +1054,12 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
         constexpr int D = decltype(d_c)::value, BITS = decltype(bits_c)::value;
         using T = decltype(zero);
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(z.wgs), dim3(kThreads), 0, stream, a, pack_view(pack));
+            hipLaunchKernelGGL(kernel, dim3(z.wgs), dim3(kThreads), 0, stream, a,
+                               static_cast<const uint8_t*>(cache->k_codes),
+                               static_cast<const uint8_t*>(cache->k_scales),
+                               static_cast<const uint8_t*>(cache->v_codes),
+                               static_cast<const uint8_t*>(cache->v_scales), page_table,
+                               pack_view(pack));
         };
         auto merge = [&](auto kernel, int rows) {
             hipLaunchKernelGGL(kernel, dim3(z.wgs * (z.rows / rows)), dim3(kThreads), 0, stream, a,
@@ -845,7 +1069,10 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
             go(mx_few_kernel<D, BITS, T>);
             merge(mx_merge_kernel<D, T, 1>, 1);
         } else {
-            go(mx_wide_kernel<D, BITS, T>);
+            const bool full = pack->bl * a.g % kWideRows == 0;
+            if (sh->page_size < kTile) go(mx_wide_kernel<D, BITS, T, false, false>);
+            else if (full && sizeof(T) == 2) go(mx_wide_kernel<D, BITS, T, true, sizeof(T) == 2>);
+            else go(mx_wide_kernel<D, BITS, T, true, false>);
             merge(mx_merge_kernel<D, T, 8>, 8);
         }
     };
