@@ -44,10 +44,10 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kTile = 32;              // keys
+constexpr int kKeys = 32;              // of a tile
 constexpr int kWideRows = 128, kFewRows = 32;
-constexpr int kStart = 5;              // what a unit's start and end cost, in key tiles
-constexpr int kLeastShare = 8;         // of a workgroup
+constexpr int kStart = 9;              // what a unit's start and end cost, in tiles
+constexpr int kLeastShare = 8;         // of a workgroup, in tiles
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleSlack = 8.0f;  // the running maximum may lag by 2^8
 
@@ -59,7 +59,7 @@ struct MxArgs {
     float* part_o;     // [2 wgs][rows][D]
     float* part_lse;   // [2 wgs][rows]
     int Hq, Hkv, g, bl, B, W_max, row_cap, wgs, ps_shift, max_pages, num_pages;
-    float scale_log2;
+    float scale_log2, slack;   // slack: of the running maximum, as a score
 };
 // What a kernel only reads, apart from its other arguments, so that the compiler may
 // use scalar loads.
@@ -92,7 +92,7 @@ struct Piece {
 template <int ROWS>
 __device__ inline int group_tiles(const MxArgs& a, const Req& r, int group) {
     const int last = min((group + 1) * ROWS, r.rows) - 1;
-    return (r.o + (last / (a.g * a.bl) + 1) * a.bl + kTile - 1) / kTile;
+    return (r.o + (last / (a.g * a.bl) + 1) * a.bl + kKeys - 1) / kKeys;
 }
 
 // Request b; `report`: an unreachable page is recorded.
@@ -113,7 +113,7 @@ __device__ inline Req request(const MxArgs& a, const PackView& pv, int b, bool r
     return r;
 }
 
-// The walk of a workgroup along its share.
+// The walk of a workgroup along its share, for units of ROWS query rows.
 template <int ROWS>
 struct Walk {
     long long at, end;    // place in the line of the present unit, end of the share
@@ -124,7 +124,7 @@ struct Walk {
 
     // The cut at place x of a unit of kt tiles, in its tiles: what is left on
     // either side is worth a piece.
-    __device__ inline int least() const { return (int)max(2LL, share / 16); }
+    __device__ inline int least() const { return (int)max(2LL, share / 32); }
     __device__ inline int cut(long long x, int kt) const {
         const int k = (int)max(0LL, min(x - kStart, (long long)kt)), m = least();
         return k < m ? 0 : kt - k < m ? kt : k;
@@ -365,7 +365,7 @@ struct Rows {
 
     // The running maximum moves when a tile's passes it by 2^8, so that results are
     // seldom rescaled; weights are up to 2^8 then.
-    __device__ inline void rescale(float mx, float scale) {
+    __device__ inline void rescale(float mx, float scale, float slack) {
         const bool need = mx > thr;
         if (__any(need)) {
             const float m_new = need ? mx * scale : m_sub;
@@ -377,7 +377,7 @@ struct Rows {
                 for (int x = 0; x < 16; ++x) o[dt][x] *= alpha;
             l *= alpha;
             m_sub = m_new;
-            if (need) thr = mx + kRescaleSlack / scale;
+            if (need) thr = mx + slack;
         }
     }
 
@@ -412,11 +412,11 @@ struct Rows {
     }
 
     // A whole tile's scores into weights, with the running statistics.
-    __device__ inline void softmax(floatx16& s, float scale, bf16x8 (&pb)[2][NP]) {
+    __device__ inline void softmax(floatx16& s, float scale, float slack, bf16x8 (&pb)[2][NP]) {
         float mx = s[0];
 #pragma unroll
         for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x]);
-        rescale(half_max(mx), scale);
+        rescale(half_max(mx), scale, slack);
         weights<16>(s, 0, scale, pb);
     }
 
@@ -445,7 +445,7 @@ struct Rows {
     // the rows that do see them get their NaN here.
     __device__ inline void spoil(const MxArgs& a, const uint8_t* vs, const int32_t* pt, int head, int key0,
                                  int end) {
-        for (int key = key0; key < min(key0 + kTile, end); ++key) {
+        for (int key = key0; key < end; ++key) {
             const int page = pt[key >> a.ps_shift];
             if ((unsigned)page >= (unsigned)a.num_pages) continue;
             const uint8_t* s = vs + ((((size_t)page * a.Hkv + head) << a.ps_shift) +
@@ -496,22 +496,11 @@ __device__ inline void store_record(const MxArgs& a, int index, const Req& r, co
 }
 
 // ------------------------------------------------------------- many rows ---
-template <int N, typename F, int... I>
-__device__ __attribute__((always_inline)) inline void static_for_impl(F& f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>{}), ...);
-}
-// f(std::integral_constant<int, 0>) ... f(std::integral_constant<int, N-1>)
-template <int N, typename F>
-__device__ __attribute__((always_inline)) inline void static_for(F&& f) {
-    static_for_impl<N>(f, std::make_integer_sequence<int, N>{});
-}
-
-// A step takes the scores of tile t + 1 on the matrix cores while the vector units
-// turn those of tile t into weights, then adds tile t's values while it looks for
-// the next scores' maximum and turns the codes of K(t + 2) and V(t + 1), loaded a
-// step before, into bf16.  Two stages of K and of V are enough then, and one
-// barrier a step.
-// PAGED: a page holds whole tiles, so a tile's loads share one scalar base.
+// A step takes a tile's scores, turns them into weights and adds its values; between
+// the products of the second half, the codes of the next tile, loaded a step before,
+// are turned into bf16 for the other stage.  The two workgroups of a CU have their
+// vector and matrix phases beside each other's.
+// PAGED: a page holds a tile, so its loads share one scalar base.
 // FULL: every wave of a unit has query rows.
 template <int D, int BITS, typename T, bool PAGED, bool FULL>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -523,8 +512,9 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     constexpr int kRowBytes = D * BITS / 8;
     using KR = KeyRows<D>;
     using VR = ValueRows<D>;
-    __shared__ __attribute__((aligned(16))) uint16_t lds_k[2][kTile * KR::kPitch];
-    __shared__ __attribute__((aligned(16))) uint16_t lds_v[2][kTile * VR::kPitch];
+    using X = Rows<D, T>;
+    __shared__ __attribute__((aligned(16))) uint16_t lds_k[2][kKeys * KR::kPitch];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_v[2][kKeys * VR::kPitch];
 
     Walk<kWideRows> walk;
     if (!walk.begin(a, pv)) return;
@@ -546,46 +536,48 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
         const int last_row = min((w.group + 1) * kWideRows, r.rows) - 1;
         const int ke = r.o + (last_row / ga + 1) * a.bl;                 // keys of the unit
         const int all = r.o + (w.group * kWideRows / ga + 1) * a.bl;     // that every row sees
-        Rows<D, T> x;
+        X x;
         x.clear();
         x.seen = r.o + (min(row, last_row) / ga + 1) * a.bl;
 
         // a thread's run of a tile: key tid / 8, elements (tid % 8) EL ...
         uint32_t kraw[CW], vraw[CW], ksc, vsc;
         bool page_err = false, bad = false;
-        auto page_of = [&](int t) { return pt[(t * kTile) >> a.ps_shift]; };   // PAGED
-        // The place of tile t among the cache's slots: of its first key (PAGED, `page` its
-        // page), of this thread's key else.  A bad page id is read as page 0.
-        auto place = [&](int t, int page) -> size_t {
-            int p = t * kTile;
+        // the page of tile t (PAGED), past the piece its last one's
+        const int k1 = w.k1;
+        auto page_of = [&](int t) {
+            return PAGED ? pt[(min(t, k1 - 1) * kKeys) >> a.ps_shift] : 0;
+        };
+        // Codes of tile t, `page` its page (PAGED).  A bad page id is read as page 0.
+        auto load_tile = [&](int t, int page) {
+            int p = t * kKeys;
             if constexpr (!PAGED) {
                 p = min(p + my_key, ke - 1);
                 page = pt[p >> a.ps_shift];
             }
             const bool good = (unsigned)page < (unsigned)a.num_pages;
             page_err |= !good;
-            return (((size_t)(good ? page : 0) * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
+            const size_t slot =
+                (((size_t)(good ? page : 0) * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
+            auto run = [&](const uint8_t* codes, const uint8_t* scales, uint32_t* raw, uint32_t& sc) {
+                if constexpr (PAGED) {
+                    // (scalar bases and a lane's 32-bit offsets: the compiler would keep
+                    // the sums of a base and the offset, 64 bits a lane)
+                    GlobalBytes c0 = (GlobalBytes)(codes + slot * kRowBytes);
+                    GlobalBytes s0 = (GlobalBytes)(scales + slot * DT);
+                    uint32_t c1 = code_at, s1 = scale_at;
+                    asm("" : "+s"(c0), "+s"(s0), "+v"(c1), "+v"(s1));
+                    load_codes<CB>(c0 + c1, raw);
+                    sc = s0[s1];
+                } else {
+                    load_codes<CB>((GlobalBytes)(codes + slot * kRowBytes + my_run * CB), raw);
+                    sc = scales[slot * DT + my_run * EL / 32];
+                }
+            };
+            run(kc, ks, kraw, ksc);
+            run(vc, vs, vraw, vsc);
         };
-        auto load_run = [&](const uint8_t* codes, const uint8_t* scales, size_t slot, uint32_t* raw,
-                            uint32_t& sc) {
-            if constexpr (PAGED) {
-                // (scalar bases and a lane's 32-bit offsets: the compiler would keep the
-                // sums of a base and the offset, 64 bits a lane)
-                GlobalBytes c0 = (GlobalBytes)(codes + slot * kRowBytes);
-                GlobalBytes s0 = (GlobalBytes)(scales + slot * DT);
-                asm("" : "+s"(c0), "+s"(s0));
-                load_codes<CB>(c0 + code_at, raw);
-                sc = s0[scale_at];
-            } else {
-                load_codes<CB>((GlobalBytes)(codes + slot * kRowBytes + my_run * CB), raw);
-                sc = scales[slot * DT + my_run * EL / 32];
-            }
-        };
-        auto load_k = [&](size_t slot) { load_run(kc, ks, slot, kraw, ksc); };
-        auto load_v = [&](size_t slot) { load_run(vc, vs, slot, vraw, vsc); };
-        // Codes into a stage.  Keys past the unit's last one have no weight, not even
-        // as NaN, and neither has a NaN value for the rows that do not see it: both
-        // become zeros (the NaN is given to those that do see it at the end).
+        // Piece i of a run into its stage.
         constexpr int NPC = EL < 8 ? 1 : EL / 8;      // pieces of a run
         auto store_piece = [&](auto rows_c, uint16_t* tile, const uint32_t* raw, uint32_t sc, int i) {
             using L = decltype(rows_c);
@@ -605,177 +597,106 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                     eight_values<BITS>(raw + i * (BITS / 4), s, true);
             }
         };
-        auto store_run = [&](auto rows_c, uint16_t* tile, const uint32_t* raw, uint32_t sc) {
-#pragma unroll
-            for (int i = 0; i < NPC; ++i) store_piece(rows_c, tile, raw, sc, i);
+        // pieces of the next tile: its values', then its keys'
+        auto stage = [&](int st, int i) {
+            if (i < NPC) store_piece(VR{}, lds_v[st], vraw, vsc, i);
+            else store_piece(KR{}, lds_k[st], kraw, ksc, i - NPC);
         };
-        auto zero_tail = [&](int t, uint32_t* raw, uint32_t& sc, bool value) {
-            if ((t + 1) * kTile <= all) return;
-            const bool past = t * kTile + my_key >= ke;
-            const bool nan = value && sc == 255;
+        // Keys past the unit's last one have no weight, not even as NaN, and neither has a
+        // NaN value for the rows that do not see it: both become zeros before they are
+        // stored (the NaN is given to those that do see it at the end).
+        auto zero_tail = [&](int t) {
+            if ((t + 1) * kKeys <= all) return;
+            const bool past = t * kKeys + my_key >= ke, nan = vsc == 255;
             bad |= nan && !past;
-            if (past || nan) {
-                sc = 127;
 #pragma unroll
-                for (int i = 0; i < CW; ++i) raw[i] = 0;
+            for (int i = 0; i < CW; ++i) {
+                kraw[i] = past ? 0 : kraw[i];
+                vraw[i] = past || nan ? 0 : vraw[i];
             }
+            ksc = past ? 127 : ksc;
+            vsc = past || nan ? 127 : vsc;
         };
-        // (tile u of the piece is tile k0 + u of the unit and lies in stage u % 2)
-        const int k0 = w.k0, nt = w.k1 - w.k0;
-        // page ids, asked for a step before the tile's codes are
-        int pg1 = PAGED ? page_of(k0 + min(1, nt - 1)) : 0, pg2 = PAGED ? page_of(k0 + min(2, nt - 1)) : 0;
-        int pg_next = PAGED ? page_of(k0 + min(3, nt - 1)) : 0;
-        size_t slot = place(k0, PAGED ? page_of(k0) : 0);   // of the next values to be loaded
-        load_k(slot);
-        load_v(slot);
+
+        load_tile(w.k0, page_of(w.k0));
+        int page = page_of(w.k0 + 1);        // asked for a step before the tile's codes are
         const T* q = static_cast<const T*>(a.q) +
                      ((size_t)(r.row0 + (row_ok ? row / a.g : 0)) * a.Hq + w.head * a.g +
                       (row_ok ? row % a.g : 0)) * D;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) query8(q + kk * 16 + h * 8, row_ok, x.qf[kk]);
-        zero_tail(k0, kraw, ksc, false);
-        store_run(KR{}, lds_k[0], kraw, ksc);
-        if (nt > 1) {
-            slot = place(k0 + 1, pg1);
-            load_k(slot);
-        }
-        __syncthreads();
-        floatx16 s_cur = floatx16{};
-        float mx = -INFINITY;
-        if (wave_ok) {
+        zero_tail(w.k0);
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds_k[0] + k_at + 16 * kk);
-#pragma unroll
-                for (int p = 0; p < NP; ++p)
-                    s_cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, x.qf[kk][p], s_cur, 0, 0, 0);
-            }
-            if ((k0 + 1) * kTile > all) x.mask(s_cur, x.seen - k0 * kTile);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s_cur[i]);
-            mx = half_max(mx);
-            x.rescale(mx, a.scale_log2);
-        }
-        zero_tail(k0, vraw, vsc, true);
-        store_run(VR{}, lds_v[0], vraw, vsc);
-        if (nt > 1) {
-            zero_tail(k0 + 1, kraw, ksc, false);
-            store_run(KR{}, lds_k[1], kraw, ksc);
-            load_v(slot);
-        }
-        if (nt > 2) {
-            slot = place(k0 + 2, pg2);
-            load_k(slot);
-        }
-        // KIND 0: a step whose loads all have tiles, which every row sees; 1: one near
-        // the end; 2: the last one
-        auto step = [&](int u, auto st_c, auto kind_c) __attribute__((always_inline)) {
+        for (int i = 0; i < 2 * NPC; ++i) stage(0, i);
+        if (w.k0 + 1 < k1) load_tile(w.k0 + 1, page);
+        page = page_of(w.k0 + 2);
+        // Tile t in stage ST.  NEAR: there may be no tile after it, and rows that do not
+        // see all of it or of the next one.
+        auto step = [&](int t, auto st_c, auto near_c) __attribute__((always_inline)) {
             constexpr int ST = decltype(st_c)::value;
-            constexpr int KIND = decltype(kind_c)::value;
-            constexpr bool LAST = KIND == 2, NEAR = KIND != 0;
-            const int t = k0 + u;
+            constexpr bool NEAR = decltype(near_c)::value;
+            constexpr int NX = DT * 2, AHEAD = 2, EVERY = NX / (2 * NPC);
+            const uint16_t* kt = lds_k[ST] + k_at;
+            auto key = [&](int i) { return *reinterpret_cast<const bf16x8*>(kt + i * 16); };
+            auto value = [&](int i) { return X::template values<VR>(lds_v[ST], i / DT, i % DT); };
             __syncthreads();
-            floatx16 s_nxt = floatx16{};
-            bf16x8 pb[2][NP];
+            bf16x8 pb[2][NP], fr[AHEAD];     // operands are read two products ahead
             if (wave_ok) {
-                constexpr int SPG = 16 / KK;
-                if constexpr (!LAST) {
-                    const uint16_t* kt = lds_k[1 - ST];
-                    bf16x8 fr[2];
-                    fr[0] = *reinterpret_cast<const bf16x8*>(kt + k_at);
-                    fr[1] = *reinterpret_cast<const bf16x8*>(kt + k_at + 16);
-                    __builtin_amdgcn_sched_barrier(0);
+                // (while one workgroup's scores run, the other's weights go behind them)
+                __builtin_amdgcn_s_setprio(1);
+                floatx16 s = floatx16{};
 #pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) {
-                        const bf16x8 kf = fr[kk & 1];
-                        if (kk + 2 < KK)
-                            fr[kk & 1] = *reinterpret_cast<const bf16x8*>(kt + k_at + 16 * (kk + 2));
-#pragma unroll
-                        for (int p = 0; p < NP; ++p)
-                            s_nxt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, x.qf[kk][p], s_nxt,
-                                                                            0, 0, 0);
-                        x.template weights<SPG>(s_cur, kk * SPG, a.scale_log2, pb);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                    if (NEAR && (t + 2) * kTile > all) x.mask(s_nxt, x.seen - (t + 1) * kTile);
-                } else {
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk)
-                        x.template weights<SPG>(s_cur, kk * SPG, a.scale_log2, pb);
-                }
-            }
-            // The codes loaded a step ago go to LDS between the products; then the next
-            // tiles' are asked for.
-            const bool more_k = !LAST && (!NEAR || u + 2 < nt);
-            if constexpr (NEAR && !LAST) {
-                zero_tail(t + 1, vraw, vsc, true);
-                if (more_k) zero_tail(t + 2, kraw, ksc, false);
-            }
-            auto stage = [&](int i) __attribute__((always_inline)) {   // i < 2 NPC
-                if constexpr (!LAST) {
-                    if (i < NPC) store_piece(VR{}, lds_v[1 - ST], vraw, vsc, i);
-                    else if (more_k) store_piece(KR{}, lds_k[ST], kraw, ksc, i - NPC);
-                }
-            };
-            if (wave_ok) {
-                constexpr int NX = DT * 2, VPG = 16 / NX, EVERY = NX / (2 * NPC);
-                const uint16_t* vt = lds_v[ST];
-                bf16x8 fr[2];
-                fr[0] = Rows<D, T>::template values<VR>(vt, 0, 0);
-                fr[1] = Rows<D, T>::template values<VR>(vt, 1 / DT, 1 % DT);
-                mx = -INFINITY;
+                for (int i = 0; i < AHEAD; ++i) fr[i] = key(i);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < NX; ++i) {
-                    const bf16x8 vf = fr[i & 1];
-                    if (i + 2 < NX)
-                        fr[i & 1] = Rows<D, T>::template values<VR>(vt, (i + 2) / DT, (i + 2) % DT);
-                    x.add(vf, i % DT, pb[i / DT]);
-                    if constexpr (!LAST) {
+                for (int i = 0; i < KK; ++i) {
+                    const bf16x8 kf = fr[i % AHEAD];
+                    fr[i % AHEAD] = i + AHEAD < KK ? key(i + AHEAD) : value(i + AHEAD - KK);
 #pragma unroll
-                        for (int y = 0; y < VPG; ++y) mx = fmaxf(mx, s_nxt[i * VPG + y]);
-                        if (i % EVERY == 0) stage(i / EVERY);
-                    }
+                    for (int p = 0; p < NP; ++p)
+                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, x.qf[i][p], s, 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-            } else {
+                __builtin_amdgcn_s_setprio(0);
+                if (NEAR && (t + 1) * kKeys > all) x.mask(s, x.seen - t * kKeys);
+                x.softmax(s, a.scale_log2, a.slack, pb);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const bool more = !NEAR || t + 1 < k1;
+            if (NEAR && more) zero_tail(t + 1);
+            if (wave_ok) {
 #pragma unroll
-                for (int i = 0; i < 2 * NPC; ++i) stage(i);
-            }
-            if constexpr (!LAST) {
-                if (more_k) load_v(slot);
-                if (!NEAR || u + 3 < nt) {
-                    slot = place(t + 3, pg_next);
-                    load_k(slot);
+                for (int i = 0; i < NX; ++i) {
+                    const bf16x8 vf = fr[i % AHEAD];
+                    if (i + AHEAD < NX) fr[i % AHEAD] = value(i + AHEAD);
+                    x.add(vf, i % DT, pb[i / DT]);
+                    if (more && i % EVERY == 0) stage(1 - ST, i / EVERY);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                if constexpr (PAGED) pg_next = page_of(k0 + min(u + 4, nt - 1));
-                if (!wave_ok) return;
-                mx = half_max(mx);
-                x.rescale(mx, a.scale_log2);
-                s_cur = s_nxt;
+            } else if (more) {
+#pragma unroll
+                for (int i = 0; i < 2 * NPC; ++i) stage(1 - ST, i);
             }
+            if (!NEAR || t + 2 < k1) load_tile(t + 2, page);
+            page = page_of(t + 3);
         };
         using C0 = std::integral_constant<int, 0>;
         using C1 = std::integral_constant<int, 1>;
-        using C2 = std::integral_constant<int, 2>;
-        // steps whose tile u + 3 is there and whose tile u + 2 every row sees
-        const int full = min(nt - 3, all / kTile - k0 - 2);
-        int u = 0;
-        for (; u + 2 <= full; u += 2) {
-            step(u, C0{}, C0{});
-            step(u + 1, C1{}, C0{});
+        // steps whose tile t + 2 is there and whose tile t + 1 every row sees
+        const int far = min(k1 - 2, all / kKeys - 1);
+        int t = w.k0;
+        for (; t + 2 <= far; t += 2) {
+            step(t, C0{}, std::false_type{});
+            step(t + 1, C1{}, std::false_type{});
         }
-        for (; u + 1 < nt; ++u) {
-            if (u & 1) step(u, C1{}, C1{});
-            else step(u, C0{}, C1{});
+        for (; t < k1; t += 2) {
+            step(t, C0{}, std::true_type{});
+            if (t + 1 < k1) step(t + 1, C1{}, std::true_type{});
         }
-        if (u & 1) step(u, C1{}, C2{});
-        else step(u, C0{}, C2{});
         if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
         // (the barrier also lets the next piece fill the stages)
         if (__syncthreads_or(bad))
-            for (int t = all / kTile; t < w.k1; ++t)
-                if (t >= k0) x.spoil(a, vs, pt, w.head, t * kTile, ke);
+            x.spoil(a, vs, pt, w.head, max(w.k0, all / kKeys) * kKeys, min(k1 * kKeys, ke));
         x.store(a, r, w, r_local, kWideRows);
         if (w.more > 0) {
             made = true;
@@ -803,7 +724,7 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     // each wave's V tile; at a piece's end the results of two waves
     constexpr int kJoin = DT * 16 * 64 * 2;   // floats
     union Lds {
-        uint16_t v[4][kTile * D];
+        uint16_t v[4][kKeys * D];
         float join[kJoin];
     };
     __shared__ __attribute__((aligned(16))) Lds lds;
@@ -839,7 +760,7 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
         uint8_t ksc[SC], vsc[SC];
         bool ok, page_err = false;
         auto load_tile = [&](int t) {
-            const int pos = t * kTile + n;
+            const int pos = t * kKeys + n;
             ok = pos < ke;
             const int p = min(pos, ke - 1);
             int page = pt[p >> a.ps_shift];
@@ -858,7 +779,7 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
         };
         if (w.k0 + wave < w.k1) load_tile(w.k0 + wave);
         for (int t = w.k0 + wave; t < w.k1; t += 4) {
-            const bool masked = (t + 1) * kTile > all;
+            const bool masked = (t + 1) * kKeys > all;
             floatx16 s = floatx16{};
             bool bad[SC];
 #pragma unroll
@@ -882,12 +803,12 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
             if (t + 4 < w.k1) load_tile(t + 4);
             wave_sync();
             bf16x8 pb[2][NP];
-            if (masked) x.mask(s, x.seen - t * kTile);
-            x.softmax(s, a.scale_log2, pb);
+            if (masked) x.mask(s, x.seen - t * kKeys);
+            x.softmax(s, a.scale_log2, a.slack, pb);
 #pragma unroll
             for (int i = 0; i < 2 * DT; ++i)
                 x.add(R::template values<TurnedRows<D>>(vt, i / DT, i % DT), i % DT, pb[i / DT]);
-            if (any_bad) x.spoil(a, vs, pt, w.head, t * kTile, ke);
+            if (any_bad) x.spoil(a, vs, pt, w.head, t * kKeys, min((t + 1) * kKeys, ke));
             wave_sync();   // the next tile's values go to the same place
         }
         if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
@@ -1049,7 +970,7 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
                    reinterpret_cast<float*>(ws + z.off_lse),
                    sh->Hq, sh->Hkv, sh->Hq / sh->Hkv, pack->bl, pack->B, pack->W_max,
                    pack->row_cap, z.wgs, log2_of(sh->page_size), sh->max_pages, sh->num_pages,
-                   scale * kLog2e};
+                   scale * kLog2e, kRescaleSlack / (scale * kLog2e)};
     auto launch = [&](auto d_c, auto bits_c, auto zero) {
         constexpr int D = decltype(d_c)::value, BITS = decltype(bits_c)::value;
         using T = decltype(zero);
@@ -1070,7 +991,7 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
             merge(mx_merge_kernel<D, T, 1>, 1);
         } else {
             const bool full = pack->bl * a.g % kWideRows == 0;
-            if (sh->page_size < kTile) go(mx_wide_kernel<D, BITS, T, false, false>);
+            if (sh->page_size < kKeys) go(mx_wide_kernel<D, BITS, T, false, false>);
             else if (full && sizeof(T) == 2) go(mx_wide_kernel<D, BITS, T, true, sizeof(T) == 2>);
             else go(mx_wide_kernel<D, BITS, T, true, false>);
             merge(mx_merge_kernel<D, T, 8>, 8);
