@@ -59,6 +59,7 @@ struct MxArgs {
     float* part_o;     // [2 wgs][rows][D]
     float* part_lse;   // [2 wgs][rows]
     int Hq, Hkv, g, bl, B, W_max, row_cap, wgs, ps_shift, max_pages, num_pages;
+    int short_line;    // the line of a full pack has fewer than 2^31 places
     float scale_log2, slack;   // slack: of the running maximum, as a score
 };
 // What a kernel only reads, apart from its other arguments, so that the compiler may
@@ -75,6 +76,12 @@ __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x);
 __device__ inline long long uniform(long long x) {
     return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 |
                        (uint32_t)uniform((int)x));
+}
+
+// A quotient of numbers that are not negative; most fit 32 bits, where a division
+// takes a third of the time.
+__device__ inline long long div_of(long long x, long long y) {
+    return ((x | y) >> 31) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
 
 // A request's part of the line.
@@ -130,32 +137,50 @@ struct Walk {
         return k < m ? 0 : kt - k < m ? kt : k;
     }
 
-    // All threads of the workgroup; false if it has no share.
-    __device__ bool begin(const MxArgs& a, const PackView& pv) {
-        __shared__ long long wave_sum[kThreads / 64];
-        __shared__ long long found[2];
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        const int per = (a.B + kThreads - 1) / kThreads;
-        long long mine = 0;
-        for (int b = tid * per; b < min((tid + 1) * per, a.B); ++b)
-            mine += (long long)a.Hkv * request<ROWS>(a, pv, b, blockIdx.x == 0).len;
-        long long sum = mine;                 // inclusive over the threads
+    // Sums of `mine` over the threads up to this one and over all.
+    template <typename Int>
+    __device__ static inline void scan(Int mine, Int& sum, Int& total) {
+        __shared__ Int wave_sum[kThreads / 64];
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        sum = mine;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
-            const long long x = __shfl_up(sum, off, 64);
+            const Int x = __shfl_up(sum, off, 64);
             if (lane >= off) sum += x;
         }
         if (lane == 63) wave_sum[wave] = sum;
         __syncthreads();
-        long long total = 0;
+        total = 0;
 #pragma unroll
         for (int i = 0; i < kThreads / 64; ++i) {
             if (i < wave) sum += wave_sum[i];
             total += wave_sum[i];
         }
-        total = uniform(total);
-        share = max((total + a.wgs - 1) / a.wgs, (long long)(kLeastShare + kStart));
-        const int busy = (int)((total + share - 1) / share);
+    }
+
+    // All threads of the workgroup; false if it has no share.
+    __device__ bool begin(const MxArgs& a, const PackView& pv) {
+        __shared__ Req found;
+        __shared__ long long found_at;
+        const int tid = threadIdx.x;
+        const int per = (a.B + kThreads - 1) / kThreads;
+        Req mine_r{};
+        long long mine = 0;
+        for (int b = tid * per; b < min((tid + 1) * per, a.B); ++b) {
+            mine_r = request<ROWS>(a, pv, b, blockIdx.x == 0);
+            mine += (long long)a.Hkv * mine_r.len;
+        }
+        long long sum, total;
+        if (a.short_line) {
+            int s, t;
+            scan((int)mine, s, t);
+            sum = s, total = uniform(t);
+        } else {
+            scan(mine, sum, total);
+            total = uniform(total);
+        }
+        share = max(div_of(total + a.wgs - 1, a.wgs), (long long)(kLeastShare + kStart));
+        const int busy = (int)div_of(total + share - 1, share);
         // Neighbours in the line read the same keys, so they belong on one XCD:
         // workgroups go to the eight in turn.
         const int each = (busy + 7) / 8;
@@ -167,19 +192,20 @@ struct Walk {
         if (sum > p && sum - mine <= p) {
             // the request that holds p is one of this thread's
             long long before = sum - mine;
-            int b = tid * per;
-            for (;; ++b) {
-                const long long len = (long long)a.Hkv * request<ROWS>(a, pv, b, false).len;
+            for (int b = tid * per; per > 1; ++b) {
+                mine_r = request<ROWS>(a, pv, b, false);
+                const long long len = (long long)a.Hkv * mine_r.len;
                 if (before + len > p) break;
                 before += len;
             }
-            found[0] = b;
-            found[1] = before;
+            found = mine_r;
+            found_at = before;
         }
         __syncthreads();
-        r = request<ROWS>(a, pv, uniform((int)found[0]), false);
-        at = uniform(found[1]);
-        head = (int)((p - at) / r.len);
+        r.b = uniform(found.b), r.row0 = uniform(found.row0), r.o = uniform(found.o);
+        r.rows = uniform(found.rows), r.groups = uniform(found.groups), r.len = uniform(found.len);
+        at = uniform(found_at);
+        head = (int)div_of(p - at, r.len);
         at += (long long)head * r.len;
         group = 0;
         for (;;) {
@@ -212,7 +238,7 @@ struct Walk {
             if (w.k0 > 0) w.first = 2 * index;
             else if (w.k1 < w.kt && w.k1 > 0) {
                 // cuts at m .. kt - m tiles of this unit, this share's end the first
-                const long long last = (at + kStart + w.kt - least()) / share;
+                const long long last = div_of(at + kStart + w.kt - least(), share);
                 w.first = 2 * index + 1;
                 w.more = (int)(last - index) + 1;
             }
@@ -325,14 +351,14 @@ __device__ inline void load_codes(GlobalBytes p, uint32_t* q) {
 #undef MX_AT
 }
 
-// Eight values from their codes (BITS / 4 dwords), zeros unless ok.
+// Eight values from their codes (BITS / 4 dwords).
 template <int BITS>
-__device__ inline u32x4 eight_values(const uint32_t* q, float scale, bool ok) {
+__device__ inline u32x4 eight_values(const uint32_t* q, float scale) {
     bf16x2 v[4];
 #pragma unroll
     for (int i = 0; i < BITS / 4; ++i) mx_dword<BITS>(q[i], scale, v + i * (16 / BITS));
-    return u32x4{ok ? __builtin_bit_cast(uint32_t, v[0]) : 0u, ok ? __builtin_bit_cast(uint32_t, v[1]) : 0u,
-                 ok ? __builtin_bit_cast(uint32_t, v[2]) : 0u, ok ? __builtin_bit_cast(uint32_t, v[3]) : 0u};
+    return u32x4{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]),
+                 __builtin_bit_cast(uint32_t, v[2]), __builtin_bit_cast(uint32_t, v[3])};
 }
 
 // --------------------------------------------------------- online softmax ---
@@ -503,7 +529,7 @@ __device__ inline void store_record(const MxArgs& a, int index, const Req& r, co
 // PAGED: a page holds a tile, so its loads share one scalar base.
 // FULL: every wave of a unit has query rows.
 template <int D, int BITS, typename T, bool PAGED, bool FULL>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2)
 mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     constexpr int EL = D / 8;             // elements of a thread's run: 8 threads to a key
     constexpr int CB = EL * BITS / 8;     // their code bytes: 2, 4, 8 or 16
@@ -594,7 +620,7 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                     u32x2{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1])};
             } else {
                 *reinterpret_cast<u32x4*>(tile + L::at(my_key, my_run * NPC + i)) =
-                    eight_values<BITS>(raw + i * (BITS / 4), s, true);
+                    eight_values<BITS>(raw + i * (BITS / 4), s);
             }
         };
         // pieces of the next tile: its values', then its keys'
@@ -756,19 +782,16 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) query8(q + kk * 8, row_ok, x.qf[kk]);
 
-        uint32_t kraw[CW], vraw[CW];
-        uint8_t ksc[SC], vsc[SC];
-        bool ok, page_err = false;
+        uint32_t kraw[CW], vraw[CW], ksc[SC], vsc[SC];
+        bool page_err = false, bad = false;
+        // Codes of this lane's half of key n of tile t.  A bad page id is read as page 0.
         auto load_tile = [&](int t) {
-            const int pos = t * kKeys + n;
-            ok = pos < ke;
-            const int p = min(pos, ke - 1);
-            int page = pt[p >> a.ps_shift];
-            if ((unsigned)page >= (unsigned)a.num_pages) {   // read as page 0
-                page_err = true;
-                page = 0;
-            }
-            const size_t slot = (((size_t)page * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
+            const int p = min(t * kKeys + n, ke - 1);
+            const int page = pt[p >> a.ps_shift];
+            const bool good = (unsigned)page < (unsigned)a.num_pages;
+            page_err |= !good;
+            const size_t slot =
+                (((size_t)(good ? page : 0) * a.Hkv + w.head) << a.ps_shift) + (p & slot_mask);
             load_codes<CB>((GlobalBytes)(kc + slot * (D * BITS / 8) + h * CB), kraw);
             load_codes<CB>((GlobalBytes)(vc + slot * (D * BITS / 8) + h * CB), vraw);
 #pragma unroll
@@ -777,40 +800,64 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                 vsc[i] = vs[slot * DT + (D >= 64 ? h * SC : 0) + i];
             }
         };
+        // As in the wide kernel: keys past the unit's last one and NaN values that not every
+        // row sees become zeros.
+        auto zero_tail = [&](int t) {
+            const bool past = t * kKeys + n >= ke;
+#pragma unroll
+            for (int i = 0; i < SC; ++i) {
+                const bool nan = vsc[i] == 255;
+                bad |= nan && !past;
+                constexpr int W = CW / SC;
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    kraw[i * W + j] = past ? 0 : kraw[i * W + j];
+                    vraw[i * W + j] = past || nan ? 0 : vraw[i * W + j];
+                }
+                ksc[i] = past ? 127 : ksc[i];
+                vsc[i] = past || nan ? 127 : vsc[i];
+            }
+        };
         if (w.k0 + wave < w.k1) load_tile(w.k0 + wave);
         for (int t = w.k0 + wave; t < w.k1; t += 4) {
             const bool masked = (t + 1) * kKeys > all;
+            if (masked) zero_tail(t);
             floatx16 s = floatx16{};
-            bool bad[SC];
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
                 constexpr int PG = D >= 64 ? 4 : KK;      // pieces of eight to a group
-                const u32x4 kf =
-                    eight_values<BITS>(kraw + kk * (BITS / 4), mx_scale(ksc[kk / PG]), ok);
+                const u32x4 kf = eight_values<BITS>(kraw + kk * (BITS / 4), mx_scale(ksc[kk / PG]));
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
                                                                 x.qf[kk][p], s, 0, 0, 0);
-                bad[kk / PG] = masked && ok && vsc[kk / PG] == 255;
                 *reinterpret_cast<u32x4*>(vt + TurnedRows<D>::at(n, h * KK + kk)) =
-                    eight_values<BITS>(vraw + kk * (BITS / 4), mx_scale(vsc[kk / PG]),
-                                       ok && !bad[kk / PG]);
+                    eight_values<BITS>(vraw + kk * (BITS / 4), mx_scale(vsc[kk / PG]));
+                __builtin_amdgcn_sched_barrier(0);   // (else every piece is in registers at once)
             }
-            bool any_bad = false;
-#pragma unroll
-            for (int i = 0; i < SC; ++i) any_bad |= bad[i];
-            any_bad = __any(any_bad);
             if (t + 4 < w.k1) load_tile(t + 4);
             wave_sync();
             bf16x8 pb[2][NP];
             if (masked) x.mask(s, x.seen - t * kKeys);
             x.softmax(s, a.scale_log2, a.slack, pb);
+            auto value = [&](int i) {
+                return R::template values<TurnedRows<D>>(vt, i / DT, i % DT);
+            };
+            bf16x8 fr[2] = {value(0), value(1)};
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < 2 * DT; ++i)
-                x.add(R::template values<TurnedRows<D>>(vt, i / DT, i % DT), i % DT, pb[i / DT]);
-            if (any_bad) x.spoil(a, vs, pt, w.head, t * kKeys, min((t + 1) * kKeys, ke));
+            for (int i = 0; i < 2 * DT; ++i) {
+                const bf16x8 v = fr[i & 1];
+                if (i + 2 < 2 * DT) fr[i & 1] = value(i + 2);
+                x.add(v, i % DT, pb[i / DT]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             wave_sync();   // the next tile's values go to the same place
         }
+        // (each wave gives its rows their NaN itself: a key is one wave's)
+        if (__any(bad))
+            for (int t = w.k0 + wave; t < w.k1; t += 4)
+                if ((t + 1) * kKeys > all) x.spoil(a, vs, pt, w.head, t * kKeys, min((t + 1) * kKeys, ke));
         if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
 
         // waves 2 and 3 join 0 and 1, then 1 joins 0
@@ -841,10 +888,12 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                 }
                 x.l = x.l * f0 + stat[to][1][lane] * f1;
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         x.o[dt][i] = x.o[dt][i] * f0 + j[(dt * 16 + i) * 64 + lane] * f1;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
         if (wave == 0) x.store(a, r, w, n, kFewRows);
@@ -941,7 +990,7 @@ MxAttnSizes mx_attention_sizes(const fb_pack* pack, const fb_attn_shape* sh, int
     MxAttnSizes z{};
     const long long most = (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv);
     z.rows = most <= kFewRows ? kFewRows : kWideRows;
-    const int per_cu = 2;   // as many as a CU holds at once
+    const int per_cu = sh->dtype == FB_BF16 && z.rows == kWideRows ? 3 : 2;   // as many as a CU holds
     z.wgs = (per_cu * (cu_count > 0 ? cu_count : 256) + 7) / 8 * 8;
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -962,6 +1011,10 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
                                const MxAttnSizes& z, hipStream_t stream) {
     const float scale = sh->sm_scale > 0.f ? sh->sm_scale : 1.0f / sqrtf((float)sh->head_dim);
     char* ws = static_cast<char*>(wsp);
+    const long long groups = ((long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv) + z.rows - 1) / z.rows;
+    const double places = (double)pack->B * sh->Hkv * groups *
+                          ((double)sh->max_pages * sh->page_size / kKeys + 1 + kStart);
+    const int short_line = places < 2147483648.0;
     const MxArgs a{q,
                    out,
                    reinterpret_cast<int32_t*>(ws + z.off_head),
@@ -970,6 +1023,7 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
                    reinterpret_cast<float*>(ws + z.off_lse),
                    sh->Hq, sh->Hkv, sh->Hq / sh->Hkv, pack->bl, pack->B, pack->W_max,
                    pack->row_cap, z.wgs, log2_of(sh->page_size), sh->max_pages, sh->num_pages,
+                   short_line,
                    scale * kLog2e, kRescaleSlack / (scale * kLog2e)};
     auto launch = [&](auto d_c, auto bits_c, auto zero) {
         constexpr int D = decltype(d_c)::value, BITS = decltype(bits_c)::value;
