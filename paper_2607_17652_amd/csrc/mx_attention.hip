@@ -46,7 +46,13 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kKeys = 32;              // of a tile
 constexpr int kWideRows = 128, kFewRows = 32;
-constexpr int kStart = 9;              // what a unit's start and end cost, in tiles
+// Caches of at most so many keys are walked by one workgroup a unit, with no merge,
+// where there are no more units than workgroups.  Divided and whole: 8 heads, one token,
+// 250 keys 13.4 and 10.9 us, 500 keys 18.2 and 12.6, 1024 keys 18.6 and 17.2; 14 units of
+// 128 rows, 700 keys 19.0 and 16.0, in float32 24.5 and 23.2.
+constexpr int kWideWholeKeys = 1024, kFewWholeKeys = 1280;
+// what a unit's start and end cost, in tiles: of 128 rows, of 32
+constexpr int kWideStart = 9, kFewStart = 20;
 constexpr int kLeastShare = 8;         // of a workgroup, in tiles
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleSlack = 8.0f;  // the running maximum may lag by 2^8
@@ -59,6 +65,7 @@ struct MxArgs {
     float* part_o;     // [2 wgs][rows][D]
     float* part_lse;   // [2 wgs][rows]
     int Hq, Hkv, g, bl, B, W_max, row_cap, wgs, ps_shift, max_pages, num_pages;
+    int whole;         // no unit is divided
     int short_line;    // the line of a full pack has fewer than 2^31 places
     float scale_log2, slack;   // slack: of the running maximum, as a score
 };
@@ -97,6 +104,9 @@ struct Piece {
 };
 
 template <int ROWS>
+constexpr int kStartOf = ROWS == kWideRows ? kWideStart : kFewStart;
+
+template <int ROWS>
 __device__ inline int group_tiles(const MxArgs& a, const Req& r, int group) {
     const int last = min((group + 1) * ROWS, r.rows) - 1;
     return (r.o + (last / (a.g * a.bl) + 1) * a.bl + kKeys - 1) / kKeys;
@@ -116,22 +126,23 @@ __device__ inline Req request(const MxArgs& a, const PackView& pv, int b, bool r
     }
     r.rows = w * a.bl * a.g;
     r.groups = (r.rows + ROWS - 1) / ROWS;
-    for (int i = 0; i < r.groups; ++i) r.len += group_tiles<ROWS>(a, r, i) + kStart;
+    for (int i = 0; i < r.groups; ++i) r.len += group_tiles<ROWS>(a, r, i) + kStartOf<ROWS>;
     return r;
 }
 
 // The walk of a workgroup along its share, for units of ROWS query rows.
 template <int ROWS>
 struct Walk {
+    static constexpr int kStart = kStartOf<ROWS>;
     long long at, end;    // place in the line of the present unit, end of the share
     long long share;
-    int index, head, group;
+    int index, head, group, whole;
     int skip;             // place of the share's start in its first unit
     Req r;
 
     // The cut at place x of a unit of kt tiles, in its tiles: what is left on
     // either side is worth a piece.
-    __device__ inline int least() const { return (int)max(2LL, share / 32); }
+    __device__ inline int least() const { return whole ? 1 << 30 : (int)max(2LL, share / 32); }
     __device__ inline int cut(long long x, int kt) const {
         const int k = (int)max(0LL, min(x - kStart, (long long)kt)), m = least();
         return k < m ? 0 : kt - k < m ? kt : k;
@@ -162,6 +173,7 @@ struct Walk {
     __device__ bool begin(const MxArgs& a, const PackView& pv) {
         __shared__ Req found;
         __shared__ long long found_at;
+        whole = a.whole;
         const int tid = threadIdx.x;
         const int per = (a.B + kThreads - 1) / kThreads;
         Req mine_r{};
@@ -182,7 +194,8 @@ struct Walk {
         share = max(div_of(total + a.wgs - 1, a.wgs), (long long)(kLeastShare + kStart));
         const int busy = (int)div_of(total + share - 1, share);
         // Neighbours in the line read the same keys, so they belong on one XCD:
-        // workgroups go to the eight in turn.
+        // workgroups go to the eight in turn (8 long requests: 435 us, 439 without;
+        // 256 requests: 777, 785).
         const int each = (busy + 7) / 8;
         index = blockIdx.x % 8 * each + blockIdx.x / 8;
         if (blockIdx.x == 0 && tid == 0) a.head[0] = busy;
@@ -668,8 +681,6 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
             __syncthreads();
             bf16x8 pb[2][NP], fr[AHEAD];     // operands are read two products ahead
             if (wave_ok) {
-                // (while one workgroup's scores run, the other's weights go behind them)
-                __builtin_amdgcn_s_setprio(1);
                 floatx16 s = floatx16{};
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) fr[i] = key(i);
@@ -683,7 +694,6 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, x.qf[i][p], s, 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_s_setprio(0);
                 if (NEAR && (t + 1) * kKeys > all) x.mask(s, x.seen - t * kKeys);
                 x.softmax(s, a.scale_log2, a.slack, pb);
                 __builtin_amdgcn_sched_barrier(0);
@@ -782,12 +792,19 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) query8(q + kk * 8, row_ok, x.qf[kk]);
 
-        uint32_t kraw[CW], vraw[CW], ksc[SC], vsc[SC];
+        // sets of codes: of the next tile, or of the next two where the registers hold them
+        constexpr int SETS = BITS == 4 && NP == 1 ? 2 : 1, STRIDE = 4 * SETS;
+        uint32_t kraws[SETS][CW], vraws[SETS][CW], kscs[SETS][SC], vscs[SETS][SC];
         bool page_err = false, bad = false;
+        // The page of key n of tile t, past the piece its last tile's.
+        auto page_of = [&](int t) {
+            return pt[min(min(t, w.k1 - 1) * kKeys + n, ke - 1) >> a.ps_shift];
+        };
         // Codes of this lane's half of key n of tile t.  A bad page id is read as page 0.
-        auto load_tile = [&](int t) {
+        auto load_tile = [&](int t, int page, int set) {
+            uint32_t(&kraw)[CW] = kraws[set], (&vraw)[CW] = vraws[set];
+            uint32_t(&ksc)[SC] = kscs[set], (&vsc)[SC] = vscs[set];
             const int p = min(t * kKeys + n, ke - 1);
-            const int page = pt[p >> a.ps_shift];
             const bool good = (unsigned)page < (unsigned)a.num_pages;
             page_err |= !good;
             const size_t slot =
@@ -802,7 +819,9 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
         };
         // As in the wide kernel: keys past the unit's last one and NaN values that not every
         // row sees become zeros.
-        auto zero_tail = [&](int t) {
+        auto zero_tail = [&](int t, int set) {
+            uint32_t(&kraw)[CW] = kraws[set], (&vraw)[CW] = vraws[set];
+            uint32_t(&ksc)[SC] = kscs[set], (&vsc)[SC] = vscs[set];
             const bool past = t * kKeys + n >= ke;
 #pragma unroll
             for (int i = 0; i < SC; ++i) {
@@ -818,10 +837,16 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                 vsc[i] = past || nan ? 127 : vsc[i];
             }
         };
-        if (w.k0 + wave < w.k1) load_tile(w.k0 + wave);
-        for (int t = w.k0 + wave; t < w.k1; t += 4) {
+        const int t0 = w.k0 + wave;
+        int page = page_of(t0 + STRIDE);          // asked for a tile before its codes are
+        if (t0 < w.k1) load_tile(t0, page_of(t0), 0);
+        if (SETS == 2 && t0 + 4 < w.k1) load_tile(t0 + 4, page_of(t0 + 4), SETS - 1);
+        auto step = [&](int t, auto set_c) __attribute__((always_inline)) {
+            constexpr int SET = decltype(set_c)::value;
+            uint32_t(&kraw)[CW] = kraws[SET], (&vraw)[CW] = vraws[SET];
+            uint32_t(&ksc)[SC] = kscs[SET], (&vsc)[SC] = vscs[SET];
             const bool masked = (t + 1) * kKeys > all;
-            if (masked) zero_tail(t);
+            if (masked) zero_tail(t, SET);
             floatx16 s = floatx16{};
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
@@ -835,7 +860,8 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                     eight_values<BITS>(vraw + kk * (BITS / 4), mx_scale(vsc[kk / PG]));
                 __builtin_amdgcn_sched_barrier(0);   // (else every piece is in registers at once)
             }
-            if (t + 4 < w.k1) load_tile(t + 4);
+            if (t + STRIDE < w.k1) load_tile(t + STRIDE, page, SET);
+            page = page_of(t + STRIDE + 4);
             wave_sync();
             bf16x8 pb[2][NP];
             if (masked) x.mask(s, x.seen - t * kKeys);
@@ -853,6 +879,10 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                 __builtin_amdgcn_sched_barrier(0);
             }
             wave_sync();   // the next tile's values go to the same place
+        };
+        for (int t = t0; t < w.k1; t += STRIDE) {
+            step(t, std::integral_constant<int, 0>{});
+            if (SETS == 2 && t + 4 < w.k1) step(t + 4, std::integral_constant<int, SETS - 1>{});
         }
         // (each wave gives its rows their NaN itself: a key is one wave's)
         if (__any(bad))
@@ -913,11 +943,10 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
 // take the pieces in turn.
 template <int D, typename T, int R>
 __global__ void __launch_bounds__(kThreads)
-mx_merge_kernel(MxArgs a, int rows) {
+mx_merge_kernel(MxArgs a, int rows, int parts) {
     constexpr int Q = D / 4, PL = kThreads / Q / R;
     __shared__ float m_of[PL][R], den_of[PL][R];
     __shared__ float4 acc_of[PL][R][Q];
-    const int parts = rows / R;
     const int i = blockIdx.x / parts, part = blockIdx.x % parts;
     if (i >= a.head[0]) return;
     const int32_t* rec = a.rec + (size_t)i * kRecInts;
@@ -1011,9 +1040,14 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
                                const MxAttnSizes& z, hipStream_t stream) {
     const float scale = sh->sm_scale > 0.f ? sh->sm_scale : 1.0f / sqrtf((float)sh->head_dim);
     char* ws = static_cast<char*>(wsp);
-    const long long groups = ((long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv) + z.rows - 1) / z.rows;
+    const long long all_rows = (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv);
+    const long long groups = (all_rows + z.rows - 1) / z.rows;
+    const long long most = all_rows < z.rows ? all_rows : z.rows;
+    const int whole = pack->B * sh->Hkv * groups <= z.wgs &&
+                      (long long)sh->max_pages * sh->page_size <=
+                          (z.rows == kFewRows ? kFewWholeKeys : kWideWholeKeys);
     const double places = (double)pack->B * sh->Hkv * groups *
-                          ((double)sh->max_pages * sh->page_size / kKeys + 1 + kStart);
+                          ((double)sh->max_pages * sh->page_size / kKeys + 1 + kFewStart);
     const int short_line = places < 2147483648.0;
     const MxArgs a{q,
                    out,
@@ -1023,7 +1057,7 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
                    reinterpret_cast<float*>(ws + z.off_lse),
                    sh->Hq, sh->Hkv, sh->Hq / sh->Hkv, pack->bl, pack->B, pack->W_max,
                    pack->row_cap, z.wgs, log2_of(sh->page_size), sh->max_pages, sh->num_pages,
-                   short_line,
+                   whole, short_line,
                    scale * kLog2e, kRescaleSlack / (scale * kLog2e)};
     auto launch = [&](auto d_c, auto bits_c, auto zero) {
         constexpr int D = decltype(d_c)::value, BITS = decltype(bits_c)::value;
@@ -1037,8 +1071,10 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
                                pack_view(pack));
         };
         auto merge = [&](auto kernel, int rows) {
-            hipLaunchKernelGGL(kernel, dim3(z.wgs * (z.rows / rows)), dim3(kThreads), 0, stream, a,
-                               z.rows);
+            if (a.whole) return;
+            const int parts = (int)((most + rows - 1) / rows);   // of the rows that a unit can have
+            hipLaunchKernelGGL(kernel, dim3(z.wgs * parts), dim3(kThreads), 0, stream, a, z.rows,
+                               parts);
         };
         if (z.rows == kFewRows) {
             go(mx_few_kernel<D, BITS, T>);

@@ -19,6 +19,7 @@ constexpr int kMxThreads = 256;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 struct MxCache {
@@ -135,6 +136,7 @@ mx_write_kernel(const T* __restrict__ k_new, const T* __restrict__ v_new, MxCach
     }
 }
 
+// Eight values, past the caches: what is read back is read next by other kernels.
 template <int BITS>
 __device__ inline void store_values(uint16_t* p, const uint32_t (&codes)[BITS / 4], float scale) {
     union {
@@ -142,70 +144,77 @@ __device__ inline void store_values(uint16_t* p, const uint32_t (&codes)[BITS / 
         u32x4 w;
     } o;
 #pragma unroll
-    for (int j = 0; j < BITS / 4; ++j) {
-        bf16x2 v[16 / BITS];
-        mx_dword<BITS>(codes[j], scale, v);
-#pragma unroll
-        for (int i = 0; i < 16 / BITS; ++i) o.v[j * (16 / BITS) + i] = v[i];
-    }
-    *reinterpret_cast<u32x4*>(p) = o.w;
+    for (int j = 0; j < BITS / 4; ++j) mx_dword<BITS>(codes[j], scale, o.v + j * (16 / BITS));
+    __builtin_nontemporal_store(o.w, reinterpret_cast<u32x4*>(p));
 }
 template <int BITS>
 __device__ inline void store_values(float* p, const uint32_t (&codes)[BITS / 4], float scale) {
-    float f[8];
+    bf16x2 v[4];
 #pragma unroll
-    for (int j = 0; j < BITS / 4; ++j) {
-        bf16x2 v[16 / BITS];
-        mx_dword<BITS>(codes[j], scale, v);
+    for (int j = 0; j < BITS / 4; ++j) mx_dword<BITS>(codes[j], scale, v + j * (16 / BITS));
 #pragma unroll
-        for (int i = 0; i < 16 / BITS; ++i) {
-            f[(j * (16 / BITS) + i) * 2] = (float)v[i][0];
-            f[(j * (16 / BITS) + i) * 2 + 1] = (float)v[i][1];
-        }
+    for (int i = 0; i < 2; ++i) {
+        const f32x4 f = {(float)v[2 * i][0], (float)v[2 * i][1], (float)v[2 * i + 1][0],
+                         (float)v[2 * i + 1][1]};
+        __builtin_nontemporal_store(f, reinterpret_cast<f32x4*>(p) + i);
     }
-    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
 }
 
 template <typename T, int BITS>
 __global__ void __launch_bounds__(kMxThreads)
 mx_read_kernel(MxCache cache, const int32_t* __restrict__ page_table,
                const int32_t* __restrict__ spans, int T_cap, T* __restrict__ k_out,
-               T* __restrict__ v_out, PackView pv, int Hkv, int D, int ps_shift, int max_pages,
-               int num_pages, int wgs) {
-    const int b = blockIdx.x / wgs, part_wg = blockIdx.x % wgs;
+               T* __restrict__ v_out, PackView pv, int Hkv, int ph_shift, int ps_shift,
+               int max_pages, int num_pages, int wgs) {
+    constexpr int U = 4;   // runs of a thread on their way
+    const int b = blockIdx.x / wgs, wg = blockIdx.x % wgs;
     const int first = spans[2 * b], n = spans[2 * b + 1];
     if (first < 0 || n < 0 || n > T_cap ||
         (long long)first + n > ((long long)max_pages << ps_shift)) {
-        if (part_wg == 0 && threadIdx.x == 0) record_error(pv.hdr, b, FB_DERR_SPAN);
+        if (wg == 0 && threadIdx.x == 0) record_error(pv.hdr, b, FB_DERR_SPAN);
         return;
     }
-    const int per_head = D / 8, per_row = Hkv * per_head;
+    // a thread's runs of eight channels lie wgs kMxThreads apart: dt positions and dat runs
+    const int per_row = Hkv << ph_shift, ph_mask = (1 << ph_shift) - 1;
+    const int stride = wgs * kMxThreads, dt = stride / per_row, dat = stride - dt * per_row;
+    const int e0 = wg * kMxThreads + threadIdx.x;
+    int t = e0 / per_row, at = e0 - t * per_row;
     const int32_t* pt = page_table + (size_t)b * max_pages;
-    const long long all = (long long)n * per_row;
-    for (long long e = (long long)part_wg * kMxThreads + threadIdx.x; e < all;
-         e += (long long)wgs * kMxThreads) {
-        const int t = (int)(e / per_row), at = (int)(e - (long long)t * per_row);
-        const int c = at / per_head, part = at - c * per_head;
-        const int pos = first + t;
-        const int page = pt[pos >> ps_shift];
-        if ((unsigned)page >= (unsigned)num_pages) {
-            if (at == 0) record_error(pv.hdr, b, FB_DERR_PAGE);
-            continue;
-        }
-        const size_t slot = (((size_t)page * Hkv + c) << ps_shift) + (pos & ((1 << ps_shift) - 1));
-        const size_t src = (slot * per_head + part) * BITS;
-        const size_t s = slot * (per_head / 4) + part / 4;
-        const size_t dst = (((size_t)b * T_cap + t) * per_row + at) * 8;
-        auto one = [&](const uint8_t* codes, const uint8_t* scales, T* out) {
-            uint32_t q[BITS / 4];
+    while (t < n) {
+        int ti[U], ai[U], page[U];
 #pragma unroll
-            for (int j = 0; j < BITS / 4; ++j)
-                q[j] = *reinterpret_cast<const uint32_t*>(codes + src + 4 * j);
-            store_values<BITS>(out + dst, q, mx_scale(scales[s]));
-        };
-        if (k_out) one(cache.kc, cache.ks, k_out);
-        if (v_out) one(cache.vc, cache.vs, v_out);
+        for (int i = 0; i < U; ++i) {
+            ti[i] = t, ai[i] = at;
+            page[i] = t < n ? pt[(first + t) >> ps_shift] : -1;
+            t += dt, at += dat;
+            if (at >= per_row) at -= per_row, ++t;
+        }
+        uint32_t kq[U][BITS / 4], vq[U][BITS / 4], ks[U], vs[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool good = (unsigned)page[i] < (unsigned)num_pages;
+            if (ti[i] < n && !good && ai[i] == 0) record_error(pv.hdr, b, FB_DERR_PAGE);
+            if (!good) ti[i] = n;   // nothing is stored
+            const int pos = first + ti[i], c = ai[i] >> ph_shift, part = ai[i] & ph_mask;
+            const size_t slot = (((size_t)(good ? page[i] : 0) * Hkv + c) << ps_shift) +
+                                (pos & ((1 << ps_shift) - 1));
+            const size_t src = ((slot << ph_shift) + part) * BITS;
+            const size_t s = (slot << (ph_shift - 2)) + part / 4;
+#pragma unroll
+            for (int j = 0; j < BITS / 4; ++j) {
+                if (k_out) kq[i][j] = *reinterpret_cast<const uint32_t*>(cache.kc + src + 4 * j);
+                if (v_out) vq[i][j] = *reinterpret_cast<const uint32_t*>(cache.vc + src + 4 * j);
+            }
+            if (k_out) ks[i] = cache.ks[s];
+            if (v_out) vs[i] = cache.vs[s];
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (ti[i] >= n) continue;
+            const size_t dst = (((size_t)b * T_cap + ti[i]) * per_row + ai[i]) * 8;
+            if (k_out) store_values<BITS>(k_out + dst, kq[i], mx_scale(ks[i]));
+            if (v_out) store_values<BITS>(v_out + dst, vq[i], mx_scale(vs[i]));
+        }
     }
 }
 
@@ -248,7 +257,7 @@ hipError_t launch_mx_read(const fb_mx_cache* cache, const int32_t* page_table,
         using T = decltype(zero);
         hipLaunchKernelGGL(kernel, dim3((unsigned)(pack->B * wgs)), dim3(kMxThreads), 0, stream,
                            cache_view(cache), page_table, spans, T_cap, static_cast<T*>(k_out),
-                           static_cast<T*>(v_out), pack_view(pack), sh->Hkv, sh->head_dim,
+                           static_cast<T*>(v_out), pack_view(pack), sh->Hkv, log2_of(sh->head_dim / 8),
                            log2_of(sh->page_size), sh->max_pages, sh->num_pages, (int)wgs);
     };
     const bool four = cache->format == FB_MX4;
