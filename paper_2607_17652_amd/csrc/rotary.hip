@@ -3,8 +3,8 @@
 //
 // rotary_kernel  a workgroup takes R packed rows: their sines and cosines go
 //                into LDS once (angles formed and reduced to [-pi, pi] in
-//                float64), then every head of q and k is turned by them, eight
-//                pairs (halves) or four (neighbours) a thread.
+//                float64), then every head of q and k is turned by them in runs of
+//                eight pairs (halves) or four (neighbours).
 #include "cache.h"
 
 namespace fb {
@@ -13,6 +13,7 @@ namespace {
 constexpr int kRotThreads = 256;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));   // anywhere
 
 struct RotArgs {
     const void *q_in, *k_in;
@@ -37,9 +38,16 @@ __device__ inline void store8(uint16_t* p, const float (&f)[8]) {
     uint16_t h[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[j] = __builtin_bit_cast(uint16_t, (__bf16)f[j]);
-    __builtin_memcpy(p, h, 16);
+    u32x4 w;
+    __builtin_memcpy(&w, h, 16);
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_at2*>(p));
 }
-__device__ inline void store8(float* p, const float (&f)[8]) { __builtin_memcpy(p, f, 32); }
+__device__ inline void store8(float* p, const float (&f)[8]) {
+    u32x4 w[2];
+    __builtin_memcpy(w, f, 32);
+    __builtin_nontemporal_store(w[0], reinterpret_cast<u32x4_at2*>(p));
+    __builtin_nontemporal_store(w[1], reinterpret_cast<u32x4_at2*>(p + 4));
+}
 __device__ inline float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 __device__ inline float load1(const float* p) { return *p; }
 __device__ inline void store1(uint16_t* p, float f) { *p = __builtin_bit_cast(uint16_t, (__bf16)f); }
@@ -71,53 +79,74 @@ rotary_kernel(RotArgs a, PackView pv) {
         rot_table[e] = make_float2(c, s);
     }
     __syncthreads();
-    // The units of a head: runs of eight pairs (the last one may be shorter), then
-    // runs of eight elements that stay.  Neighbours lie four pairs to a run.
-    const int turned = HALVES ? (np + 7) / 8 : (2 * np + 7) / 8;
-    const int rest0 = HALVES ? 2 * np : turned * 8;      // elements from here on stay
-    const int units = turned + (a.D - rest0 + 7) / 8;
-    const int heads = (a.q_in ? a.Hq : 0) + (a.k_in ? a.Hkv : 0);
-    const int qh = a.q_in ? a.Hq : 0;
-    for (int e = threadIdx.x; e < rows * heads * units; e += kRotThreads) {
-        const int rh = e / units, u = e - rh * units;
-        const int i = rh / heads, h = rh - i * heads;
-        const int row = row0 + i;
-        if (pv.row_req[row] < 0) continue;
-        const bool is_q = h < qh;
-        const size_t at = is_q ? ((size_t)row * a.Hq + h) * a.D
-                               : ((size_t)row * a.Hkv + (h - qh)) * a.D;
-        const T* in = static_cast<const T*>(is_q ? a.q_in : a.k_in) + at;
-        T* out = static_cast<T*>(is_q ? a.q_out : a.k_out) + at;
-        const float2* cs = rot_table + i * np;
-        if (u >= turned) {
-            const int d0 = rest0 + (u - turned) * 8;
-            if (in == out) continue;
-            for (int d = d0; d < min(d0 + 8, a.D); ++d) out[d] = in[d];
-        } else if constexpr (HALVES) {
-            const int j0 = u * 8;
-            if (j0 + 8 <= np) {
-                float lo[8], hi[8];
-                load8(in + j0, lo);
-                load8(in + np + j0, hi);
+    const int qh = a.q_in ? a.Hq : 0, heads = qh + (a.k_in ? a.Hkv : 0);
+    // element 0 of head rh % heads of row rh / heads, and its table
+    struct Head {
+        const T* in;
+        T* out;
+        int table;
+    };
+    auto head_of = [&](int rh) {
+        const int i = rh / heads, h = rh - i * heads, row = row0 + i;
+        const size_t at = h < qh ? ((size_t)row * a.Hq + h) * a.D
+                                 : ((size_t)row * a.Hkv + (h - qh)) * a.D;
+        return Head{static_cast<const T*>(h < qh ? a.q_in : a.k_in) + at,
+                    static_cast<T*>(h < qh ? a.q_out : a.k_out) + at,
+                    pv.row_req[row] < 0 ? -1 : i * np};
+    };
+    // Runs of eight pairs (halves) or of four (neighbours; the last one's may be fewer), U
+    // of them on their way to a thread.
+    constexpr int U = sizeof(T) == 2 ? 2 : 1, N = HALVES ? 2 : 1;
+    const int runs = HALVES ? np / 8 : (2 * np + 7) / 8, all = rows * heads * runs;
+    for (int e0 = threadIdx.x; e0 < all; e0 += U * kRotThreads) {
+        Head hd[U];
+        int u[U];
+        float f[U][N][8];
 #pragma unroll
-                for (int x = 0; x < 8; ++x) turn(lo[x], hi[x], cs[j0 + x]);
-                store8(out + j0, lo);
-                store8(out + np + j0, hi);
-            } else {
-                for (int j = j0; j < np; ++j) {
-                    float x = load1(in + j), y = load1(in + np + j);
-                    turn(x, y, cs[j]);
-                    store1(out + j, x);
-                    store1(out + np + j, y);
-                }
+        for (int k = 0; k < U; ++k) {
+            const int e = e0 + k * kRotThreads, rh = e / runs;
+            if (e >= all) {
+                hd[k].table = -1;
+                continue;
             }
-        } else {
-            float f[8];
-            load8(in + u * 8, f);
+            hd[k] = head_of(rh);
+            u[k] = e - rh * runs;
+            if (hd[k].table < 0) continue;
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                if (u * 4 + x < np) turn(f[2 * x], f[2 * x + 1], cs[u * 4 + x]);
-            store8(out + u * 8, f);
+            for (int y = 0; y < N; ++y) load8(hd[k].in + u[k] * 8 + y * np, f[k][y]);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (hd[k].table < 0) continue;
+            const float2* cs = rot_table + hd[k].table;
+            if constexpr (HALVES) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) turn(f[k][0][x], f[k][1][x], cs[u[k] * 8 + x]);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (u[k] * 4 + x < np) turn(f[k][0][2 * x], f[k][0][2 * x + 1], cs[u[k] * 4 + x]);
+            }
+#pragma unroll
+            for (int y = 0; y < N; ++y) store8(hd[k].out + u[k] * 8 + y * np, f[k][y]);
+        }
+    }
+    // What runs of eight leave over: up to seven pairs (halves), and elements that stay.
+    const int pairs = HALVES ? np - runs * 8 : 0;
+    const int rest0 = HALVES ? 2 * np : runs * 8, left = pairs + a.D - rest0;
+    for (int e = threadIdx.x; e < rows * heads * left; e += kRotThreads) {
+        const int rh = e / left, x = e - rh * left;
+        const Head hd = head_of(rh);
+        if (hd.table < 0) continue;
+        if (x < pairs) {
+            const int j = runs * 8 + x;
+            float p = load1(hd.in + j), q = load1(hd.in + np + j);
+            turn(p, q, rot_table[hd.table + j]);
+            store1(hd.out + j, p);
+            store1(hd.out + np + j, q);
+        } else if (hd.in != hd.out) {
+            const int d = rest0 + x - pairs;
+            hd.out[d] = hd.in[d];
         }
     }
 }
