@@ -113,7 +113,8 @@ int fb_mx_write_window_kv(const void* k_new, const void* v_new,
  * and values: position first_b + t goes to row t of request b.  The values that
  * the codes stand for are exact in both dtypes.
  *   spans         int32[B][2]: first_b and n_b, 0 <= first_b, 0 <= n_b <= T,
- *                 first_b + n_b <= max_pages * page_size
+ *                 first_b + n_b <= max_pages * page_size and below 2^31
+ *   T             at most 2^30
  *   k_out, v_out  [B][T][Hkv][d] (dtype of sh), 16-byte aligned; either may be
  *                 NULL, not both; rows from n_b on are not written
  *   pack          its B, and the status word; what it holds is not read
@@ -139,9 +140,12 @@ size_t fb_mx_attention_workspace_bytes(const fb_pack* pack, const fb_attn_shape*
  *   q, out  [row_cap][Hq][d] (dtype of sh), 16-byte aligned; out may be q
  *   ws      device workspace of fb_mx_attention_workspace_bytes bytes, 16-byte
  *           aligned
- * Deterministic; kv_split as for fb_wavefront_attention.  A NaN scale spoils
- * the rows that see its key, no others.  A page id outside [0, num_pages) is
- * recorded as FB_DERR_PAGE and the rows of its request hold no result. */
+ * Deterministic: repeated calls give bit-identical results.  How long contexts
+ * are divided among workgroups, and so the rounding of a request's rows, goes
+ * by the whole pack; kv_split is not read.  A NaN scale spoils the rows that see
+ * its key, no others.  A page id outside [0, num_pages) is recorded as
+ * FB_DERR_PAGE and the rows of its request hold no result; a window that the
+ * page table does not reach is recorded too, and its request skipped. */
 int fb_mx_attention(const void* q, const fb_mx_cache* cache,
                     const int32_t* page_table, const fb_pack* pack,
                     const fb_attn_shape* sh, void* out, void* ws,

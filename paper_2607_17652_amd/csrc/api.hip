@@ -897,6 +897,17 @@ namespace {
 
 static size_t elt_bytes(const fb_attn_shape* sh) { return sh->dtype == FB_BF16 ? 2 : 4; }
 
+static int check_cache_shape(const fb_pack* pack, const fb_attn_shape* sh) {
+    const int rc = check_heads_and_pages(sh);
+    if (rc) return rc;
+    // the kernels count a block's runs of eight channels and a window's query rows in 32 bits
+    const long long row = ((long long)sh->Hq + sh->Hkv) * (sh->head_dim / 8);
+    if (row * 16 >= 1LL << 31 || (long long)pack->bl * sh->Hkv * (sh->head_dim / 8) >= 1LL << 31 ||
+        (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv) >= 1LL << 31)
+        return fail(FB_E_UNSUPPORTED, "too many heads for this pack");
+    return FB_OK;
+}
+
 static int check_mx_cache(const fb_mx_cache* c, const int32_t* page_table) {
     if (!c) return fail(FB_E_INVAL, "cache is NULL");
     if (c->format != FB_MX4 && c->format != FB_MX8)
@@ -916,7 +927,7 @@ int fb_rotary_axes(const void* q_in, void* q_out, const void* k_in, void* k_out,
                    const fb_rotary* rotary, void* stream) {
     int rc = check_pack(pack);
     if (rc) return rc;
-    rc = check_heads_and_pages(sh);
+    rc = check_cache_shape(pack, sh);
     if (rc) return rc;
     if (!rotary) return fail(FB_E_INVAL, "rotary is NULL");
     if (rotary->n_axes < 1 || rotary->n_axes > 8)
@@ -956,7 +967,7 @@ int fb_mx_write_window_kv(const void* k_new, const void* v_new, const fb_mx_cach
                           const fb_attn_shape* sh, void* stream) {
     int rc = check_pack(pack);
     if (rc) return rc;
-    rc = check_heads_and_pages(sh);
+    rc = check_cache_shape(pack, sh);
     if (rc) return rc;
     rc = check_mx_cache(cache, page_table);
     if (rc) return rc;
@@ -974,11 +985,12 @@ int fb_mx_read_kv(const fb_mx_cache* cache, const int32_t* page_table, const int
                   void* stream) {
     int rc = check_pack(pack);
     if (rc) return rc;
-    rc = check_heads_and_pages(sh);
+    rc = check_cache_shape(pack, sh);
     if (rc) return rc;
     rc = check_mx_cache(cache, page_table);
     if (rc) return rc;
     if (T < 1) return fail(FB_E_INVAL, "T must be >= 1");
+    if (T > 1 << 30) return fail(FB_E_UNSUPPORTED, "T %d above 2^30", T);
     if (!spans || !aligned(spans, 4))
         return fail(FB_E_INVAL, "spans must be a 4-byte aligned pointer");
     if (!k_out && !v_out) return fail(FB_E_INVAL, "neither k_out nor v_out");
@@ -993,7 +1005,7 @@ int fb_mx_read_kv(const fb_mx_cache* cache, const int32_t* page_table, const int
 }
 
 size_t fb_mx_attention_workspace_bytes(const fb_pack* pack, const fb_attn_shape* sh) {
-    if (check_pack(pack) || check_heads_and_pages(sh)) return 0;
+    if (check_pack(pack) || check_cache_shape(pack, sh)) return 0;
     return fb::mx_attention_sizes(pack, sh, cu_count()).total;
 }
 
@@ -1002,7 +1014,7 @@ int fb_mx_attention(const void* q, const fb_mx_cache* cache, const int32_t* page
                     size_t ws_bytes, void* stream) {
     int rc = check_pack(pack);
     if (rc) return rc;
-    rc = check_heads_and_pages(sh);
+    rc = check_cache_shape(pack, sh);
     if (rc) return rc;
     rc = check_mx_cache(cache, page_table);
     if (rc) return rc;

@@ -65,6 +65,7 @@ struct MxArgs {
     float* part_o;     // [2 wgs][rows][D]
     float* part_lse;   // [2 wgs][rows]
     int Hq, Hkv, g, bl, B, W_max, row_cap, wgs, ps_shift, max_pages, num_pages;
+    int max_keys;      // that the page table reaches
     int whole;         // no unit is divided
     int short_line;    // the line of a full pack has fewer than 2^31 places
     float scale_log2, slack;   // slack: of the running maximum, as a score
@@ -120,7 +121,7 @@ __device__ inline Req request(const MxArgs& a, const PackView& pv, int b, bool r
     if (w <= 0 || w > a.W_max || row0 < 0 || row0 > a.row_cap - w * a.bl) return r;
     r.row0 = row0;
     r.o = pv.row_pos[row0];
-    if ((long long)r.o + (long long)w * a.bl > ((long long)a.max_pages << a.ps_shift) || r.o < 0) {
+    if (r.o < 0 || (long long)r.o + (long long)w * a.bl > a.max_keys) {
         if (report) record_error(pv.hdr, b, FB_DERR_PAGE);
         return r;
     }
@@ -1043,11 +1044,13 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
     const long long all_rows = (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv);
     const long long groups = (all_rows + z.rows - 1) / z.rows;
     const long long most = all_rows < z.rows ? all_rows : z.rows;
-    const int whole = pack->B * sh->Hkv * groups <= z.wgs &&
-                      (long long)sh->max_pages * sh->page_size <=
-                          (z.rows == kFewRows ? kFewWholeKeys : kWideWholeKeys);
+    // (positions are 32-bit; the last ones are left out, so that tiles end within them)
+    long long max_keys = (long long)sh->max_pages * sh->page_size;
+    if (max_keys > 0x7fffffffLL - 4096) max_keys = 0x7fffffffLL - 4096;
+    const int whole = (long long)pack->B * sh->Hkv * groups <= z.wgs &&
+                      max_keys <= (z.rows == kFewRows ? kFewWholeKeys : kWideWholeKeys);
     const double places = (double)pack->B * sh->Hkv * groups *
-                          ((double)sh->max_pages * sh->page_size / kKeys + 1 + kFewStart);
+                          ((double)max_keys / kKeys + 1 + kFewStart);
     const int short_line = places < 2147483648.0;
     const MxArgs a{q,
                    out,
@@ -1057,7 +1060,7 @@ hipError_t launch_mx_attention(const void* q, const fb_mx_cache* cache, const in
                    reinterpret_cast<float*>(ws + z.off_lse),
                    sh->Hq, sh->Hkv, sh->Hq / sh->Hkv, pack->bl, pack->B, pack->W_max,
                    pack->row_cap, z.wgs, log2_of(sh->page_size), sh->max_pages, sh->num_pages,
-                   whole, short_line,
+                   (int)max_keys, whole, short_line,
                    scale * kLog2e, kRescaleSlack / (scale * kLog2e)};
     auto launch = [&](auto d_c, auto bits_c, auto zero) {
         constexpr int D = decltype(d_c)::value, BITS = decltype(bits_c)::value;

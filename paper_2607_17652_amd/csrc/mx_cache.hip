@@ -169,25 +169,29 @@ mx_read_kernel(MxCache cache, const int32_t* __restrict__ page_table,
     constexpr int U = 4;   // runs of a thread on their way
     const int b = blockIdx.x / wgs, wg = blockIdx.x % wgs;
     const int first = spans[2 * b], n = spans[2 * b + 1];
-    if (first < 0 || n < 0 || n > T_cap ||
+    if (first < 0 || n < 0 || n > T_cap || (long long)first + n > 0x7fffffffLL ||
         (long long)first + n > ((long long)max_pages << ps_shift)) {
         if (wg == 0 && threadIdx.x == 0) record_error(pv.hdr, b, FB_DERR_SPAN);
         return;
     }
-    // a thread's runs of eight channels lie wgs kMxThreads apart: dt positions and dat runs
-    const int per_row = Hkv << ph_shift, ph_mask = (1 << ph_shift) - 1;
-    const int stride = wgs * kMxThreads, dt = stride / per_row, dat = stride - dt * per_row;
+    // Runs of eight channels go head by head of G positions each, so that a wave reads
+    // neighbouring keys; a thread's lie wgs kMxThreads apart: dg groups and dat runs.
+    constexpr int kG = 2;   // log2 of G
+    const int per_row = Hkv << ph_shift, per_group = per_row << kG, ph_mask = (1 << ph_shift) - 1;
+    const int stride = wgs * kMxThreads, dg = stride / per_group, dat = stride - dg * per_group;
     const int e0 = wg * kMxThreads + threadIdx.x;
-    int t = e0 / per_row, at = e0 - t * per_row;
+    int grp = e0 / per_group, at = e0 - grp * per_group;
     const int32_t* pt = page_table + (size_t)b * max_pages;
-    while (t < n) {
-        int ti[U], ai[U], page[U];
+    while (grp << kG < n) {
+        int ti[U], ai[U], page[U];   // position, run of its row, page
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            ti[i] = t, ai[i] = at;
+            const int t = (grp << kG) + ((at >> ph_shift) & ((1 << kG) - 1));
+            ti[i] = t;
+            ai[i] = (at >> (ph_shift + kG) << ph_shift) + (at & ph_mask);
             page[i] = t < n ? pt[(first + t) >> ps_shift] : -1;
-            t += dt, at += dat;
-            if (at >= per_row) at -= per_row, ++t;
+            grp += dg, at += dat;
+            if (at >= per_group) at -= per_group, ++grp;
         }
         uint32_t kq[U][BITS / 4], vq[U][BITS / 4], ks[U], vs[U];
 #pragma unroll

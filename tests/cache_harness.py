@@ -10,15 +10,15 @@ from tail_harness import TORCH, Batch, f64
 EPS = 2.0 ** -24
 
 
-def table(bt, ps, seed, spare=2):
-    """A page table whose rows cover each request's window, in shuffled pages; what it
-    does not need holds a page id out of range."""
+def table(bt, ps, seed, spare=2, reach=0):
+    """A page table whose rows cover each request's window, in shuffled pages, and reach
+    `reach` keys at least; what it does not need holds a page id out of range."""
     rng = np.random.default_rng(seed)
     w = bt.state["R"] - bt.state["L"]
     need = -(-(bt.o + w * bt.bl) // ps)
     pages = int(need.sum()) + spare
     ids = rng.permutation(pages)
-    t = np.full((bt.B, int(need.max()) + 1), pages + 7, dtype=np.int32)
+    t = np.full((bt.B, max(int(need.max()) + 1, -(-reach // ps))), pages + 7, dtype=np.int32)
     at = 0
     for b, n in enumerate(need):
         t[b, :n] = ids[at:at + n]
@@ -30,11 +30,11 @@ class Cache:
     """A cache of `bits` for the batch, filled with codes and scales that are anything
     the format can hold (no NaN), a power of two around 2^spread."""
 
-    def __init__(self, bt, Hq, Hkv, d, ps, bits, dtype, seed=0, spread=0):
+    def __init__(self, bt, Hq, Hkv, d, ps, bits, dtype, seed=0, spread=0, reach=0):
         rng = np.random.default_rng(seed)
         self.bt, self.bits, self.Hq, self.Hkv, self.d, self.ps = bt, bits, Hq, Hkv, d, ps
         self.dtype = dtype
-        self.table, self.pages = table(bt, ps, seed)
+        self.table, self.pages = table(bt, ps, seed, reach=reach)
         shape = (self.pages, Hkv, ps)
         n = d * bits // 8
         self.host = []

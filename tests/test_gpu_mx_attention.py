@@ -12,9 +12,10 @@ pytestmark = pytest.mark.gpu
 
 
 class Attend:
-    def __init__(self, bt, Hq, Hkv, d, ps, bits, dtype, seed=0, scale=0.0, size=1.0, cache=None):
+    def __init__(self, bt, Hq, Hkv, d, ps, bits, dtype, seed=0, scale=0.0, size=1.0, cache=None,
+                 reach=0):
         self.bt = bt
-        self.c = c = Cache(bt, Hq, Hkv, d, ps, bits, dtype, seed=seed) if cache is None else cache
+        self.c = c = cache or Cache(bt, Hq, Hkv, d, ps, bits, dtype, seed=seed, reach=reach)
         if cache is None:
             c.cuda()
         c.shape.sm_scale = scale
@@ -75,14 +76,33 @@ def test_batches(batch, Hq, Hkv, d, ps, dtype, bits):
     assert status(bt.pack) == (0, -1)
 
 
+LONG = 5000      # a page table of so many keys: contexts are divided, however short they are
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,ps", [(128, 32), (64, 8), (32, 64)])
+@pytest.mark.parametrize("Hq", [2, 24])
+def test_short_contexts_under_long_tables(Hq, d, ps, dtype, bits):
+    bt = Batch(w=[2, 1, 3], o=[700, 31, 1100], bl=5, W_max=3).cuda()
+    a = Attend(bt, Hq, 2, d, ps, bits, dtype, seed=d, reach=LONG)
+    a.run()
+    a.check()
+    again = torch.full_like(a.out, 7)
+    a.ws.fill_(0xff)
+    a.run(again)
+    assert torch.equal(again, a.out)
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [0, 1, 31, 32, 33, 63, 64, 95, 127, 128, 129, 255, 257, 1000, 4093])
 def test_one_token_after_prefixes_of_every_length(n, dtype, bits):
     bt = Batch(w=[1], o=[n], bl=1, W_max=1).cuda()
-    a = Attend(bt, 8, 2, 64, 16, bits, dtype, seed=n)
-    a.run()
-    a.check()
+    for reach in (0, LONG):
+        a = Attend(bt, 8, 2, 64, 16, bits, dtype, seed=n, reach=reach)
+        a.run()
+        a.check()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
