@@ -766,6 +766,10 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     };
     __shared__ __attribute__((aligned(16))) Lds lds;
     __shared__ float stat[2][2][64];
+    // fp32: the rows' three parts, the same for every wave; in registers they would spill
+    // (64 single tokens over long contexts: 529 us, 234 so)
+    constexpr bool kQueryInLds = NP == 3;
+    __shared__ __attribute__((aligned(16))) u32x4 lds_q[kQueryInLds ? KK : 1][NP][64];
 
     Walk<kFewRows> walk;
     if (!walk.begin(a, pv)) return;
@@ -791,7 +795,22 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                      ((size_t)(r.row0 + (row_ok ? row / a.g : 0)) * a.Hq + w.head * a.g +
                       (row_ok ? row % a.g : 0)) * D + h * (D / 2);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) query8(q + kk * 8, row_ok, x.qf[kk]);
+        for (int kk = 0; kk < KK; ++kk) {
+            if constexpr (kQueryInLds) {
+                if (kk % 4 != wave) continue;
+                bf16x8 f[NP];
+                query8(q + kk * 8, row_ok, f);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) lds_q[kk][p][lane] = __builtin_bit_cast(u32x4, f[p]);
+            } else {
+                query8(q + kk * 8, row_ok, x.qf[kk]);
+            }
+        }
+        if constexpr (kQueryInLds) __syncthreads();
+        auto query = [&](int kk, int p) {
+            if constexpr (kQueryInLds) return __builtin_bit_cast(bf16x8, lds_q[kk][p][lane]);
+            else return x.qf[kk][p];
+        };
 
         // sets of codes: of the next tile, or of the next two where the registers hold them
         constexpr int SETS = BITS == 4 && NP == 1 ? 2 : 1, STRIDE = 4 * SETS;
@@ -856,7 +875,7 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                                x.qf[kk][p], s, 0, 0, 0);
+                                                                query(kk, p), s, 0, 0, 0);
                 *reinterpret_cast<u32x4*>(vt + TurnedRows<D>::at(n, h * KK + kk)) =
                     eight_values<BITS>(vraw + kk * (BITS / 4), mx_scale(vsc[kk / PG]));
                 __builtin_amdgcn_sched_barrier(0);   // (else every piece is in registers at once)
