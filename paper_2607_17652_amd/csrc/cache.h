@@ -40,11 +40,9 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// A scale byte as the float it stands for (2^(code - 127), NaN for 255; codes
-// below 1 are not written).
-__device__ inline float mx_scale(uint32_t code) {
-    return __uint_as_float(code == 255u ? 0x7fc00000u : code << 23);
-}
+// A scale byte as the conversions below take it: they read the exponent alone, and make
+// NaN of everything where it is 255.
+__device__ inline float mx_scale(uint32_t code) { return __uint_as_float(code << 23); }
 
 // Two elements of a dword of codes, as bf16, which holds them exactly (two or
 // four significant bits): pair I of four in E2M1, of two in E4M3.

@@ -561,8 +561,8 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int my_key = tid >> 3, my_run = tid & 7;
     const int slot_mask = (1 << a.ps_shift) - 1;
-    const uint32_t code_at = my_key * kRowBytes + my_run * CB;
-    const uint32_t scale_at = my_key * DT + my_run * EL / 32;
+    uint32_t code_at = my_key * kRowBytes + my_run * CB;
+    uint32_t scale_at = my_key * DT + my_run * EL / 32;
     const int k_at = KR::at(n, h);        // a key operand's piece 2 kk + h lies 16 kk on
     bool made = false;        // a unit that this share begins and does not end
     Piece w;
@@ -605,10 +605,9 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                     // the sums of a base and the offset, 64 bits a lane)
                     GlobalBytes c0 = (GlobalBytes)(codes + slot * kRowBytes);
                     GlobalBytes s0 = (GlobalBytes)(scales + slot * DT);
-                    uint32_t c1 = code_at, s1 = scale_at;
-                    asm("" : "+s"(c0), "+s"(s0), "+v"(c1), "+v"(s1));
-                    load_codes<CB>(c0 + c1, raw);
-                    sc = s0[s1];
+                    asm("" : "+s"(c0), "+s"(s0), "+v"(code_at), "+v"(scale_at));
+                    load_codes<CB>(c0 + code_at, raw);
+                    sc = s0[scale_at];
                 } else {
                     load_codes<CB>((GlobalBytes)(codes + slot * kRowBytes + my_run * CB), raw);
                     sc = scales[slot * DT + my_run * EL / 32];
