@@ -707,6 +707,9 @@ def fb_mx_read_kv(cache, page_table, spans, k_out, v_out, pack, shape, stream=No
     be None)."""
     out = k_out if k_out is not None else v_out
     T = 0 if out is None else out.shape[1]
+    if k_out is not None and v_out is not None and v_out.shape[1] != T:
+        raise FlowBlockError(FB_E_INVAL, f"k_out {tuple(k_out.shape)} and v_out "
+                                         f"{tuple(v_out.shape)} differ")
     t, n = _type(shape.dtype), pack.B * T * shape.Hkv * shape.head_dim
     _check(lib().fb_mx_read_kv(*_mx_cache(cache, page_table, pack, shape),
                                _dense(spans, _type(FB_I32), 2 * pack.B, "spans"), T,

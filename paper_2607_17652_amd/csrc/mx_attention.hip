@@ -17,11 +17,21 @@
 // workgroup finds its place in the line from the requests' windows alone.  A
 // unit that a cut divides is merged afterwards.
 //   mx_wide_kernel   groups of 128 rows, 32 to a wave; the waves share a key
-//                    tile, which they turn into bf16 in LDS
+//                    tile, which they turn into bf16 in LDS.  Bound by the
+//                    issue of matrix and vector instructions together: 87
+//                    vector instructions (16 of them conversions of codes) to
+//                    16 products, the matrix cores busy 46% of the time.  256
+//                    requests, 20416 rows over 128 .. 8192 keys, 4 bits: 763 us,
+//                    880 TFLOP/s; 8 requests over 16K .. 32K keys, 8 bits: 424
+//                    us, 940 TFLOP/s, which is what the same attention over a
+//                    bf16 cache reaches
 //   mx_few_kernel    requests of at most 32 rows (single tokens among them):
 //                    the waves take key tiles in turn, each for all rows, and
-//                    join at the end; no tile is shared, so no wave waits
-//   mx_merge_kernel  the divided units' pieces, by their log-sum-exps
+//                    join at the end; no tile is shared, so no wave waits.  Bound
+//                    by memory where the contexts are long: 64 tokens over 1K ..
+//                    32K keys, 639 MB in 4 bits, 140 us, 4.6 TB/s; in 8 bits 1.2
+//                    GB in 245 us, 5.0 TB/s
+//   mx_merge_kernel  the divided units' pieces, by their log-sum-exps (6 .. 15 us)
 //
 // S^T = K Q^T leaves in lane l the scores of query row l % 32 and keys
 // 8 (x / 4) + 4 (l / 32) + x % 4, x < 16.  The product O^T += V^T P^T takes the
@@ -52,6 +62,7 @@ constexpr int kWideRows = 128, kFewRows = 32;
 // 128 rows, 700 keys 19.0 and 16.0, in float32 24.5 and 23.2.
 constexpr int kWideWholeKeys = 1024, kFewWholeKeys = 1280;
 // what a unit's start and end cost, in tiles: of 128 rows, of 32
+// (256 requests of windows: 4 798 us, 9 777, 14 804; 64 single tokens: 14 154, 20 152, 40 158)
 constexpr int kWideStart = 9, kFewStart = 20;
 constexpr int kLeastShare = 8;         // of a workgroup, in tiles
 constexpr float kLog2e = 1.4426950408889634f;
@@ -142,7 +153,7 @@ struct Walk {
     Req r;
 
     // The cut at place x of a unit of kt tiles, in its tiles: what is left on
-    // either side is worth a piece.
+    // either side is worth a piece (a 32nd of a share; an eighth costs 2%).
     __device__ inline int least() const { return whole ? 1 << 30 : (int)max(2LL, share / 32); }
     __device__ inline int cut(long long x, int kt) const {
         const int k = (int)max(0LL, min(x - kStart, (long long)kt)), m = least();
@@ -237,8 +248,19 @@ struct Walk {
         for (;;) {
             if (at >= end) return false;
             while (r.len == 0 || head >= a.Hkv) {
-                if (r.b + 1 >= a.B) return false;
-                r = request<ROWS>(a, pv, r.b + 1, false);
+                int b = r.b + 1;
+                if (r.len == 0) {
+                    // (one that has no rows: the next that has, 64 at a look)
+                    const int lane = threadIdx.x & 63;
+                    uint64_t live = 0;
+                    for (; b < a.B; b += 64) {
+                        live = __ballot(b + lane < a.B && pv.req_w[min(b + lane, a.B - 1)] > 0);
+                        if (live) break;
+                    }
+                    if (live) b += __ffsll((unsigned long long)live) - 1;
+                }
+                if (b >= a.B) return false;
+                r = request<ROWS>(a, pv, uniform(b), false);
                 head = 0;
             }
             w.head = head;
@@ -538,8 +560,11 @@ __device__ inline void store_record(const MxArgs& a, int index, const Req& r, co
 // ------------------------------------------------------------- many rows ---
 // A step takes a tile's scores, turns them into weights and adds its values; between
 // the products of the second half, the codes of the next tile, loaded a step before,
-// are turned into bf16 for the other stage.  The two workgroups of a CU have their
-// vector and matrix phases beside each other's.
+// are turned into bf16 for the other stage.  The three workgroups of a CU have their
+// vector and matrix phases beside each other's; taking the next tile's scores beside
+// this one's weights within a wave needs registers for two workgroups only and was
+// slower (256 requests 850 us, 820 so with two, 780 with three), with 64 keys a step
+// too.  The order is held by scheduling barriers: left to the compiler it cost 1-2%.
 // PAGED: a page holds a tile, so its loads share one scalar base.
 // FULL: every wave of a unit has query rows.
 template <int D, int BITS, typename T, bool PAGED, bool FULL>
@@ -1038,7 +1063,8 @@ MxAttnSizes mx_attention_sizes(const fb_pack* pack, const fb_attn_shape* sh, int
     MxAttnSizes z{};
     const long long most = (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv);
     z.rows = most <= kFewRows ? kFewRows : kWideRows;
-    const int per_cu = sh->dtype == FB_BF16 && z.rows == kWideRows ? 3 : 2;   // as many as a CU holds
+    // as many as a CU holds at once: by their registers
+    const int per_cu = sh->dtype == FB_BF16 && z.rows == kWideRows ? 3 : 2;
     z.wgs = (per_cu * (cu_count > 0 ? cu_count : 256) + 7) / 8 * 8;
     size_t off = 0;
     auto take = [&](size_t bytes) {

@@ -9,7 +9,14 @@
 //
 // mx_write_kernel  a lane takes eight channels of a key and of a value; four
 //                  lanes share a group and find its maximum by lane moves.
-// mx_read_kernel   the same eight channels a lane on the way back.
+//                  Bound by memory: 20416 rows of 8 heads of 128 in bf16, 106 MB
+//                  in 20.4 us, 5.2 TB/s, a large copy's rate.
+// mx_read_kernel   the same eight channels a lane on the way back, four runs at a
+//                  time.  Bound by memory, four bytes written to one read in 4
+//                  bits: 8 prefixes of 16K .. 32K keys of 8 heads of 128, 980 MB
+//                  in 201 us from memory, 4.9 TB/s (231 with whole rows of heads
+//                  instead of neighbouring keys to a wave, 240 without the hint on
+//                  the stores), 146 where the memory-side cache holds the codes.
 #include "cache.h"
 
 namespace fb {

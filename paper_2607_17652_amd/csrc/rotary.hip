@@ -4,7 +4,11 @@
 // rotary_kernel  a workgroup takes R packed rows: their sines and cosines go
 //                into LDS once (angles formed and reduced to [-pi, pi] in
 //                float64), then every head of q and k is turned by them in runs of
-//                eight pairs (halves) or four (neighbours).
+//                eight pairs (halves) or four (neighbours).  Bound by memory: 20416
+//                rows of 32 + 8 heads of 128 in bf16, 421 MB in 81 us from memory,
+//                5.2 TB/s, a large copy's rate; 71.5 on the same rows again, where
+//                it took 112 with plain stores and 87 with one run at a time.  Four
+//                rows to a workgroup: two 124, eight 118 (plain stores, of 112).
 #include "cache.h"
 
 namespace fb {

@@ -80,6 +80,12 @@ def test_codes_of_another_width_are_too_few(pack):
             shape(BF), Null)
 
 
+def test_read_outputs_of_other_lengths(pack):
+    t = [device(B, n, HKV, D, dtype=BF) for n in (T, T + 1)]
+    refused("differ", fb.fb_mx_read_kv, cache(4), device(B, MP, dtype=I32), device(B, 2, dtype=I32), *t, pack,
+            shape(BF), Null)
+
+
 @pytest.mark.parametrize("dtype,other", [(BF, F32), (F32, BF)])
 def test_rotary(pack, dtype, other):
     floats = dict(q_in=(ROWS, HQ, D), q_out=(ROWS, HQ, D), k_in=(ROWS, HKV, D), k_out=(ROWS, HKV, D))

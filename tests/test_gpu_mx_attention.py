@@ -122,6 +122,10 @@ def test_groups_of_rows(w, bl, g, dtype):
                                    dict(w=[2, 1, 3] * 30, o=list(range(7, 4507, 50)), bl=32, W_max=3),
                                    dict(w=[1] * 300, o=[(i * 37) % 90 for i in range(300)], bl=1, W_max=1,
                                         inactive=tuple(range(5, 300, 7))),
+                                   dict(w=[1] * 300, o=[(i * 53) % 400 for i in range(300)], bl=1, W_max=1,
+                                        inactive=tuple(i for i in range(300) if i not in (3, 4, 150, 299))),
+                                   dict(w=[2] * 200, o=[(i * 53) % 400 for i in range(200)], bl=20, W_max=2,
+                                        layout="padded", inactive=tuple(i for i in range(200) if i % 66)),
                                    dict(w=[1, 2], o=[20000, 11], bl=16, W_max=2, layout="padded"),
                                    dict(w=[1], o=[70000], bl=1, W_max=1)])
 def test_shares_that_cut_units_anywhere(batch):
