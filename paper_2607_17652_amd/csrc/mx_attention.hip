@@ -783,10 +783,9 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     using R = Rows<D, T>;
     constexpr int KK = R::KK, DT = R::DT, NP = R::NP;
     // each wave's V tile; at a piece's end the results of two waves
-    constexpr int kJoin = DT * 16 * 64 * 2;   // floats
     union Lds {
         uint16_t v[4][kKeys * D];
-        float join[kJoin];
+        float4 join[2][DT * 4][64];
     };
     __shared__ __attribute__((aligned(16))) Lds lds;
     __shared__ float stat[2][2][64];
@@ -940,14 +939,16 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
             __syncthreads();
             const bool gives = wave >= from && wave < 2 * from;
             const int to = wave & (from - 1);
-            float* j = lds.join + to * (kJoin / 2);
+            float4(&j)[DT * 4][64] = lds.join[to];
             if (gives) {
                 stat[to][0][lane] = x.thr == -INFINITY ? -INFINITY : x.m_sub;
                 stat[to][1][lane] = x.l;
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) j[(dt * 16 + i) * 64 + lane] = x.o[dt][i];
+                for (int i = 0; i < DT * 4; ++i) {
+                    const floatx16& o = x.o[i / 4];
+                    const int at = i % 4 * 4;
+                    j[i][lane] = make_float4(o[at], o[at + 1], o[at + 2], o[at + 3]);
+                }
             }
             __syncthreads();
             if (wave < from) {
@@ -962,11 +963,15 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                 }
                 x.l = x.l * f0 + stat[to][1][lane] * f1;
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        x.o[dt][i] = x.o[dt][i] * f0 + j[(dt * 16 + i) * 64 + lane] * f1;
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int i = 0; i < DT * 4; ++i) {
+                    floatx16& o = x.o[i / 4];
+                    const int at = i % 4 * 4;
+                    const float4 v = j[i][lane];
+                    o[at] = o[at] * f0 + v.x * f1;
+                    o[at + 1] = o[at + 1] * f0 + v.y * f1;
+                    o[at + 2] = o[at + 2] * f0 + v.z * f1;
+                    o[at + 3] = o[at + 3] * f0 + v.w * f1;
+                    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }

@@ -105,14 +105,15 @@ def test_one_token_after_prefixes_of_every_length(n, dtype, bits):
         a.check()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype,d,ps,bits", [("bf16", 64, 16, 4), ("f32", 64, 16, 4), ("bf16", 128, 32, 8),
+                                             ("f32", 128, 64, 8)])
 @pytest.mark.parametrize("w,bl,g", [(1, 32, 1), (1, 33, 1), (4, 8, 1), (1, 1, 32), (1, 1, 33), (4, 32, 4),
                                     (3, 43, 1), (2, 64, 1), (2, 65, 1), (5, 13, 3), (6, 1, 5)])
-def test_groups_of_rows(w, bl, g, dtype):
+def test_groups_of_rows(w, bl, g, dtype, d, ps, bits):
     """Rows on both sides of a wave's 32 and a workgroup's 128, blocks that end inside
     groups, and windows whose blocks see different tiles."""
     bt = Batch(w=[w, max(1, w - 1)], o=[45, 300], bl=bl, W_max=w).cuda()
-    a = Attend(bt, 2 * g, 2, 64, 16, 4, dtype, seed=bl)
+    a = Attend(bt, 2 * g, 2, d, ps, bits, dtype, seed=bl)
     a.run()
     rng = np.random.default_rng(w)
     a.check(rows=np.unique(np.append(rng.integers(0, len(bt.live), 40), [0, len(bt.live) - 1])))
@@ -128,10 +129,11 @@ def test_groups_of_rows(w, bl, g, dtype):
                                         layout="padded", inactive=tuple(i for i in range(200) if i % 66)),
                                    dict(w=[1, 2], o=[20000, 11], bl=16, W_max=2, layout="padded"),
                                    dict(w=[1], o=[70000], bl=1, W_max=1)])
-def test_shares_that_cut_units_anywhere(batch):
+@pytest.mark.parametrize("d,ps,bits", [(64, 16, 4), (128, 32, 8), (32, 64, 4)])
+def test_shares_that_cut_units_anywhere(batch, d, ps, bits):
     """Few and many units, long beside short ones, more requests than threads."""
     bt = Batch(**batch).cuda()
-    a = Attend(bt, 8, 2, 64, 16, 4, "bf16", seed=3)
+    a = Attend(bt, 8, 2, d, ps, bits, "bf16", seed=3, reach=LONG)
     a.run()
     rng = np.random.default_rng(1)
     a.check(rows=np.unique(rng.integers(0, len(bt.live), 24)))
