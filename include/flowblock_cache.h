@@ -77,7 +77,9 @@ int fb_rotary_axes(const void* q_in, void* q_out, const void* k_in, void* k_out,
  * bits, 52% in 8.  Codes are 16-byte aligned, scales need no alignment.
  * Scales of 2 .. 252 (FB_MX4) or 10 .. 246 (FB_MX8) keep every value normal and
  * finite in bf16, and fb_mx_write_window_kv writes no others, but for 255: its
- * 32 values are NaN. */
+ * 32 values are NaN.  In a cache that others have filled, values under 2^-126 may
+ * be taken as 0, values past bf16's largest are infinite, and E4M3's own NaN codes
+ * (127, 255), which are not written here, may spoil every row of the request. */
 typedef struct fb_mx_cache {
     void* k_codes;
     void* k_scales;

@@ -65,6 +65,11 @@ constexpr int kWideWholeKeys = 1024, kFewWholeKeys = 1280;
 // (256 requests of windows: 4 798 us, 9 777, 14 804; 64 single tokens: 14 154, 20 152, 40 158)
 constexpr int kWideStart = 9, kFewStart = 20;
 constexpr int kLeastShare = 8;         // of a workgroup, in tiles
+// Workgroups of a CU: as many as their registers let it hold at once.  (Heads of 32 with
+// one fewer: 8 long requests 186 us, 175 so; 64 single tokens in 8 bits 74, 63.5.)
+constexpr int per_cu(int D, bool bf16, int rows) {
+    return !bf16 ? 2 : rows == kWideRows ? (D == 32 ? 4 : 3) : (D == 32 ? 3 : 2);
+}
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleSlack = 8.0f;  // the running maximum may lag by 2^8
 
@@ -568,7 +573,7 @@ __device__ inline void store_record(const MxArgs& a, int index, const Req& r, co
 // PAGED: a page holds a tile, so its loads share one scalar base.
 // FULL: every wave of a unit has query rows.
 template <int D, int BITS, typename T, bool PAGED, bool FULL>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, per_cu(D, sizeof(T) == 2, kWideRows))
 mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     constexpr int EL = D / 8;             // elements of a thread's run: 8 threads to a key
     constexpr int CB = EL * BITS / 8;     // their code bytes: 2, 4, 8 or 16
@@ -775,7 +780,7 @@ __device__ inline void wave_sync() {
 }
 
 template <int D, int BITS, typename T>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, per_cu(D, sizeof(T) == 2, kFewRows))
 mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
     constexpr int CB = D / 2 * BITS / 8;   // code bytes of half a key: a lane's
     constexpr int CW = CB / 4;
@@ -1068,9 +1073,8 @@ MxAttnSizes mx_attention_sizes(const fb_pack* pack, const fb_attn_shape* sh, int
     MxAttnSizes z{};
     const long long most = (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv);
     z.rows = most <= kFewRows ? kFewRows : kWideRows;
-    // as many as a CU holds at once: by their registers
-    const int per_cu = sh->dtype == FB_BF16 && z.rows == kWideRows ? 3 : 2;
-    z.wgs = (per_cu * (cu_count > 0 ? cu_count : 256) + 7) / 8 * 8;
+    const int each = per_cu(sh->head_dim, sh->dtype == FB_BF16, z.rows);
+    z.wgs = (each * (cu_count > 0 ? cu_count : 256) + 7) / 8 * 8;
     size_t off = 0;
     auto take = [&](size_t bytes) {
         const size_t at = off;
