@@ -969,6 +969,9 @@ int fb_mx_write_window_kv(const void* k_new, const void* v_new, const fb_mx_cach
     if (rc) return rc;
     rc = check_cache_shape(pack, sh);
     if (rc) return rc;
+    if ((long long)pack->bl * sh->Hkv * (sh->head_dim / 8) > fb::kMxWriteRuns)
+        return fail(FB_E_UNSUPPORTED, "a block of %d tokens of %d heads of %d is too large", pack->bl,
+                    sh->Hkv, sh->head_dim);
     rc = check_mx_cache(cache, page_table);
     if (rc) return rc;
     if (!k_new || !v_new) return fail(FB_E_INVAL, "a tensor pointer is NULL");

@@ -11,6 +11,10 @@ namespace fb {
 hipError_t launch_rotary(const void* q_in, void* q_out, const void* k_in, void* k_out,
                          const int32_t* positions, const fb_pack* pack, const fb_attn_shape* sh,
                          const fb_rotary* rotary, hipStream_t stream);
+// The write's threads count a block's runs of eight channels in 32 bits and step past the
+// last one by the grid's width, of at most kMxWriteTall workgroups a block.
+constexpr int kMxThreads = 256, kMxWriteTall = 65535;
+constexpr long long kMxWriteRuns = (1LL << 31) - (long long)kMxWriteTall * kMxThreads;
 hipError_t launch_mx_write(const void* k_new, const void* v_new, const fb_mx_cache* cache,
                            const int32_t* page_table, const fb_pack* pack,
                            const fb_attn_shape* sh, hipStream_t stream);

@@ -22,8 +22,6 @@
 namespace fb {
 namespace {
 
-constexpr int kMxThreads = 256;
-
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -236,7 +234,7 @@ hipError_t launch_mx_write(const void* k_new, const void* v_new, const fb_mx_cac
                            const fb_attn_shape* sh, hipStream_t stream) {
     const long long n = (long long)pack->bl * sh->Hkv * (sh->head_dim / 8);
     const long long wgs = (n + kMxThreads - 1) / kMxThreads;
-    const dim3 grid(pack->tile_cap, (unsigned)(wgs < 65535 ? wgs : 65535));
+    const dim3 grid(pack->tile_cap, (unsigned)(wgs < kMxWriteTall ? wgs : kMxWriteTall));
     auto go = [&](auto kernel, auto zero) {
         using T = decltype(zero);
         hipLaunchKernelGGL(kernel, grid, dim3(kMxThreads), 0, stream,
