@@ -135,21 +135,23 @@ rotary_kernel(RotArgs a, PackView pv) {
             for (int y = 0; y < N; ++y) store8(hd[k].out + u[k] * 8 + y * np, f[k][y]);
         }
     }
-    // What runs of eight leave over: up to seven pairs (halves), and elements that stay.
-    const int pairs = HALVES ? np - runs * 8 : 0;
-    const int rest0 = HALVES ? 2 * np : runs * 8, left = pairs + a.D - rest0;
-    for (int e = threadIdx.x; e < rows * heads * left; e += kRotThreads) {
-        const int rh = e / left, x = e - rh * left;
-        const Head hd = head_of(rh);
+    // What runs of eight leave over: up to seven pairs (halves), and elements that stay.  (Counted
+    // without a sign: four rows' elements may pass 2^31, where heads d < 2^30.)
+    const uint32_t pairs = HALVES ? np - runs * 8 : 0;
+    const uint32_t rest0 = HALVES ? 2 * np : runs * 8, left = pairs + a.D - rest0;
+    const uint32_t over = (uint32_t)rows * heads * left;
+    for (uint32_t e = threadIdx.x; e < over; e += kRotThreads) {
+        const uint32_t rh = e / left, x = e - rh * left;
+        const Head hd = head_of((int)rh);
         if (hd.table < 0) continue;
         if (x < pairs) {
-            const int j = runs * 8 + x;
+            const uint32_t j = runs * 8 + x;
             float p = load1(hd.in + j), q = load1(hd.in + np + j);
             turn(p, q, rot_table[hd.table + j]);
             store1(hd.out + j, p);
             store1(hd.out + np + j, q);
         } else if (hd.in != hd.out) {
-            const int d = rest0 + x - pairs;
+            const uint32_t d = rest0 + x - pairs;
             hd.out[d] = hd.in[d];
         }
     }

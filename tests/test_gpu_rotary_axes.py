@@ -131,3 +131,31 @@ def test_many_rows():
                       fb.make_rotary(freq, axis))
     check(bt, q, qo, pos, freq, axis, "halves", "bf16")
     check(bt, k, ko, pos, freq, axis, "halves", "bf16")
+
+
+@pytest.mark.parametrize("pairing", ["halves", "neighbours"])
+def test_elements_that_stay_past_31_bits(pairing):
+    """One pair of heads of 128, and so many heads that four rows' other elements are more
+    than 2^31: all of them are there, and the pairs turned."""
+    H, d, rows = 4_300_000, 128, 4
+    if pairing == "neighbours":            # a run of four pairs takes six of them along
+        H = 4_500_000
+    assert rows * H * (d - (8 if pairing == "neighbours" else 2)) > 1 << 31
+    bt = Batch(w=[1], o=[5], bl=rows, W_max=1).cuda()
+    q = torch.empty(rows, H, d, dtype=torch.int16, device="cuda").random_(0x3000, 0x4100) \
+        .view(torch.bfloat16)              # 2^-31 .. 8, and their negatives
+    q[..., ::3] *= -1
+    out = torch.zeros_like(q)
+    pos = torch.tensor([[0, 1, 2, 3]], dtype=torch.int32, device="cuda")
+    fb.fb_rotary_axes(q, out, None, None, pos, bt.pack, fb.make_shape(H, 1, d, "bf16", 8, 1, 1),
+                      fb.make_rotary([0.5], [0], pairing))
+    for r in range(rows):
+        assert torch.equal(out[r, :, 2:].view(torch.int16), q[r, :, 2:].view(torch.int16))
+        for i in range(0, H, 1 << 20):
+            a, b = (q[r, i:i + (1 << 20), j].double() for j in (0, 1))
+            c, s = np.cos(0.5 * r), np.sin(0.5 * r)
+            mag = (a.abs() + b.abs()) * 12 * EPS
+            for got, want in ((out[r, i:i + (1 << 20), 0], a * c - b * s),
+                              (out[r, i:i + (1 << 20), 1], b * c + a * s)):
+                tol = mag + want.abs() * HALF_STEP["bf16"] * (1 + 2 ** -6)
+                assert ((got.double() - want).abs() <= tol).all()
