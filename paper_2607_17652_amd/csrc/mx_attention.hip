@@ -111,7 +111,7 @@ __device__ inline long long div_of(long long x, long long y) {
 // A request's part of the line.
 struct Req {
     int b, row0, o, rows, groups;
-    int len;           // of one KV head
+    long long len;     // of one KV head (65536 groups over 1M keys pass 2^31)
 };
 
 // A piece of a unit: key tiles [k0, k1) of kt.
@@ -197,7 +197,7 @@ struct Walk {
         long long mine = 0;
         for (int b = tid * per; b < min((tid + 1) * per, a.B); ++b) {
             mine_r = request<ROWS>(a, pv, b, blockIdx.x == 0);
-            mine += (long long)a.Hkv * mine_r.len;
+            mine += a.Hkv * mine_r.len;
         }
         long long sum, total;
         if (a.short_line) {
@@ -224,7 +224,7 @@ struct Walk {
             long long before = sum - mine;
             for (int b = tid * per; per > 1; ++b) {
                 mine_r = request<ROWS>(a, pv, b, false);
-                const long long len = (long long)a.Hkv * mine_r.len;
+                const long long len = a.Hkv * mine_r.len;
                 if (before + len > p) break;
                 before += len;
             }
@@ -236,7 +236,7 @@ struct Walk {
         r.rows = uniform(found.rows), r.groups = uniform(found.groups), r.len = uniform(found.len);
         at = uniform(found_at);
         head = (int)div_of(p - at, r.len);
-        at += (long long)head * r.len;
+        at += head * r.len;
         group = 0;
         for (;;) {
             const int len = group_tiles<ROWS>(a, r, group) + kStart;
