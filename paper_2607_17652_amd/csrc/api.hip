@@ -900,10 +900,11 @@ static size_t elt_bytes(const fb_attn_shape* sh) { return sh->dtype == FB_BF16 ?
 static int check_cache_shape(const fb_pack* pack, const fb_attn_shape* sh) {
     const int rc = check_heads_and_pages(sh);
     if (rc) return rc;
-    // the kernels count a block's runs of eight channels and a window's query rows in 32 bits
+    // the kernels count a block's runs of eight channels and a window's query rows, the end of
+    // their last group of 128 among them, in 32 bits
     const long long row = ((long long)sh->Hq + sh->Hkv) * (sh->head_dim / 8);
     if (row * 16 >= 1LL << 31 || (long long)pack->bl * sh->Hkv * (sh->head_dim / 8) >= 1LL << 31 ||
-        (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv) >= 1LL << 31)
+        (long long)pack->W_max * pack->bl * (sh->Hq / sh->Hkv) > (1LL << 31) - 128)
         return fail(FB_E_UNSUPPORTED, "too many heads for this pack");
     return FB_OK;
 }

@@ -36,3 +36,20 @@ def test_write_takes_blocks_below(lib, bl, Hkv, d):
     refused(lib, "INVAL", lib.fb_mx_write_window_kv(at(1), at(2, 1), cache(), at(14),
                                                     packed(lib, 1, 1, bl),
                                                     shape(Hq=Hkv, Hkv=Hkv, head_dim=d), None))
+
+
+@pytest.mark.parametrize("W,bl,g", [(9, 119304647, 2), (1, 119304647, 18), (2, 151, 7110873)])
+def test_attention_refuses_windows_whose_last_group_passes_31_bits(lib, W, bl, g):
+    """Groups of 128 rows: the last one's end has to be below 2^31."""
+    assert (1 << 31) - 128 < W * bl * g < 1 << 31
+    h, s = packed(lib, 1, W, bl), shape(Hq=g, Hkv=1, head_dim=32)
+    assert lib.fb_mx_attention_workspace_bytes(h, s) == 0
+    refused(lib, "UNSUPPORTED", lib.fb_mx_attention(at(1), cache(), at(14), h, s, at(2), at(3), BIG,
+                                                    None))
+
+
+@pytest.mark.parametrize("W,bl,g", [(1, (1 << 24) - 1, 128), (64, 1 << 17, 255), (2, 1 << 23, 127)])
+def test_attention_takes_windows_below(lib, W, bl, g):
+    assert W * bl * g <= (1 << 31) - 128
+    assert lib.fb_mx_attention_workspace_bytes(packed(lib, 1, W, bl),
+                                               shape(Hq=g, Hkv=1, head_dim=32)) > 0
