@@ -145,7 +145,8 @@ size_t fb_mx_attention_workspace_bytes(const fb_pack* pack, const fb_attn_shape*
  * Deterministic: repeated calls give bit-identical results.  How long contexts
  * are divided among workgroups, and so the rounding of a request's rows, goes
  * by the whole pack; kv_split is not read.  A NaN scale spoils the rows that see
- * its key, no others.  A page id outside [0, num_pages) is recorded as
+ * its key, no others; an infinite value makes its channel infinite or NaN in
+ * those rows, and nothing else.  A page id outside [0, num_pages) is recorded as
  * FB_DERR_PAGE and the rows of its request hold no result; a window that the
  * page table does not reach is recorded too, and its request skipped. */
 int fb_mx_attention(const void* q, const fb_mx_cache* cache,

@@ -67,5 +67,15 @@ __device__ inline void mx_dword(uint32_t codes, float scale, bf16x2* v) {
     }
 }
 
+// Scales that the write makes end here; in a group of a higher one (255 is NaN) the codes
+// whose magnitudes are mx_infinite's or more pass bf16's largest.
+template <int BITS>
+constexpr uint32_t kMxHighest = BITS == 4 ? 252 : 246;
+// E2M1: 4 2^126 and 2 2^127 are 2^128; E4M3: (1 + m/8) 2^(x-7) 2^(scale-127) with x >= 262 - scale
+template <int BITS>
+__device__ inline uint32_t mx_infinite(uint32_t scale) {
+    return BITS == 4 ? (scale == 253 ? 6 : 4) : (262 - scale) << 3;
+}
+
 }  // namespace
 }  // namespace fb

@@ -402,6 +402,26 @@ __device__ inline u32x4 eight_values(const uint32_t* q, float scale) {
                  __builtin_bit_cast(uint32_t, v[2]), __builtin_bit_cast(uint32_t, v[3])};
 }
 
+// Zeros in place of the infinite values of a dword of codes; bits of them where there were
+// any.  All codes at once: a magnitude with the sign's bit set, less the first infinite one,
+// keeps that bit where it is as large.
+template <int BITS>
+__device__ inline uint32_t drop_infinite(uint32_t& q, uint32_t scale) {
+    constexpr uint32_t kOnes = BITS == 4 ? 0x11111111u : 0x01010101u, kSigns = kOnes << (BITS - 1);
+    const uint32_t high = ((q | kSigns) - mx_infinite<BITS>(scale) * kOnes) & kSigns;
+    q &= ~((high << 1) - (high >> (BITS - 1)));
+    return high;
+}
+
+// The lane's number, formed anew where it is asked for: what follows from it behind the
+// tiles' loop would else be formed in front of it and take the loop's registers (windows
+// over 8 bits 824 us, 836 so).
+__device__ inline int late_lane() {
+    int lane;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(lane));
+    return lane;
+}
+
 // --------------------------------------------------------- online softmax ---
 // A wave's 32 query rows: lane l has row l % 32, half of its scores and of its
 // result's channels.
@@ -508,27 +528,45 @@ struct Rows {
             o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k], o[dt], 0, 0, 0);
     }
 
-    // Values of NaN scales in a tile that not every row sees were staged as zeros:
-    // the rows that do see them get their NaN here.
-    __device__ inline void spoil(const MxArgs& a, const uint8_t* vs, const int32_t* pt, int head, int key0,
-                                 int end) {
+    // Values of NaN scales and infinite ones in a tile that not every row sees were staged as
+    // zeros: the rows that do see them get their NaN or infinity here.
+    template <int BITS>
+    __device__ inline void spoil(const MxArgs& a, const uint8_t* vc, const uint8_t* vs,
+                                 const int32_t* pt, int head, int key0, int end) {
+        const int h = late_lane() >> 5;
         for (int key = key0; key < end; ++key) {
             const int page = pt[key >> a.ps_shift];
             if ((unsigned)page >= (unsigned)a.num_pages) continue;
-            const uint8_t* s = vs + ((((size_t)page * a.Hkv + head) << a.ps_shift) +
-                                       (key & ((1 << a.ps_shift) - 1))) * DT;
+            const size_t slot = (((size_t)page * a.Hkv + head) << a.ps_shift) +
+                                (key & ((1 << a.ps_shift) - 1));
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-                if (s[dt] == 255 && key < seen)
+            for (int dt = 0; dt < DT; ++dt) {
+                const uint32_t s = vs[slot * DT + dt];
+                if (s <= kMxHighest<BITS> || key >= seen) continue;
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) o[dt][x] = __uint_as_float(0x7fc00000u);
+                for (int x = 0; x < 16; x += 4) {      // four neighbouring channels
+                    const uint8_t* at = vc + (slot * D + dt * 32 + 2 * x + 4 * h) * BITS / 8;
+                    const uint32_t four = BITS == 4 ? *reinterpret_cast<const uint16_t*>(at)
+                                                    : *reinterpret_cast<const uint32_t*>(at);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t code = four >> i * BITS & ((1u << BITS) - 1);
+                        const uint32_t mag = code & ((1u << (BITS - 1)) - 1);
+                        if (s == 255 || (BITS == 8 && mag == 127))
+                            o[dt][x + i] = __uint_as_float(0x7fc00000u);
+                        else if (mag >= mx_infinite<BITS>(s))
+                            o[dt][x + i] += mag == code ? INFINITY : -INFINITY;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);   // (rare: registers count, not time)
+                }
+            }
         }
     }
 
     // The rows' results, or their piece's.
-    __device__ inline void store(const MxArgs& a, const Req& r, const Piece& w, int r_local,
+    __device__ inline void store(const MxArgs& a, const Req& r, const Piece& w, int row0,
                                  int row_stride) {
-        const int h = (threadIdx.x >> 5) & 1;
+        const int lane = late_lane(), h = lane >> 5, r_local = row0 + (lane & 31);
         const float sum = l + __shfl_xor(l, 32, 64);
         const int row = w.group * row_stride + r_local;
         if (row >= r.rows) return;
@@ -672,8 +710,8 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
             else store_piece(KR{}, lds_k[st], kraw, ksc, i - NPC);
         };
         // Keys past the unit's last one have no weight, not even as NaN, and neither has a
-        // NaN value for the rows that do not see it: both become zeros before they are
-        // stored (the NaN is given to those that do see it at the end).
+        // NaN or infinite value for the rows that do not see it: both become zeros before they
+        // are stored (those that do see it get it at the end).
         auto zero_tail = [&](int t) {
             if ((t + 1) * kKeys <= all) return;
             const bool past = t * kKeys + my_key >= ke, nan = vsc == 255;
@@ -685,6 +723,9 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
             }
             ksc = past ? 127 : ksc;
             vsc = past || nan ? 127 : vsc;
+            if (vsc > kMxHighest<BITS>)
+#pragma unroll
+                for (int i = 0; i < CW; ++i) bad |= drop_infinite<BITS>(vraw[i], vsc) != 0;
         };
 
         load_tile(w.k0, page_of(w.k0));
@@ -762,8 +803,8 @@ mx_wide_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
         if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
         // (the barrier also lets the next piece fill the stages)
         if (__syncthreads_or(bad))
-            x.spoil(a, vs, pt, w.head, max(w.k0, all / kKeys) * kKeys, min(k1 * kKeys, ke));
-        x.store(a, r, w, r_local, kWideRows);
+            x.template spoil<BITS>(a, vc, vs, pt, w.head, max(w.k0, all / kKeys) * kKeys, min(k1 * kKeys, ke));
+        x.store(a, r, w, uniform(wave) * 32, kWideRows);
         if (w.more > 0) {
             made = true;
             if (tid == 0) store_record(a, walk.index, r, w, kWideRows);
@@ -865,8 +906,8 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                 vsc[i] = vs[slot * DT + (D >= 64 ? h * SC : 0) + i];
             }
         };
-        // As in the wide kernel: keys past the unit's last one and NaN values that not every
-        // row sees become zeros.
+        // As in the wide kernel: keys past the unit's last one, and NaN and infinite values that
+        // not every row sees, become zeros.
         auto zero_tail = [&](int t, int set) {
             uint32_t(&kraw)[CW] = kraws[set], (&vraw)[CW] = vraws[set];
             uint32_t(&ksc)[SC] = kscs[set], (&vsc)[SC] = vscs[set];
@@ -883,6 +924,9 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                 }
                 ksc[i] = past ? 127 : ksc[i];
                 vsc[i] = past || nan ? 127 : vsc[i];
+                if (vsc[i] > kMxHighest<BITS>)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) bad |= drop_infinite<BITS>(vraw[i * W + j], vsc[i]) != 0;
             }
         };
         const int t0 = w.k0 + wave;
@@ -932,10 +976,11 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
             step(t, std::integral_constant<int, 0>{});
             if (SETS == 2 && t + 4 < w.k1) step(t + 4, std::integral_constant<int, SETS - 1>{});
         }
-        // (each wave gives its rows their NaN itself: a key is one wave's)
+        // (each wave gives its rows theirs itself: a key is one wave's)
         if (__any(bad))
             for (int t = w.k0 + wave; t < w.k1; t += 4)
-                if ((t + 1) * kKeys > all) x.spoil(a, vs, pt, w.head, t * kKeys, min((t + 1) * kKeys, ke));
+                if ((t + 1) * kKeys > all)
+                    x.template spoil<BITS>(a, vc, vs, pt, w.head, t * kKeys, min((t + 1) * kKeys, ke));
         if (page_err) record_error(pv.hdr, r.b, FB_DERR_PAGE);
 
         // waves 2 and 3 join 0 and 1, then 1 joins 0
@@ -980,7 +1025,7 @@ mx_few_kernel(MxArgs a, MX_CACHE_PARAMS, PackView pv) {
                 }
             }
         }
-        if (wave == 0) x.store(a, r, w, n, kFewRows);
+        if (wave == 0) x.store(a, r, w, 0, kFewRows);
         if (w.more > 0) {
             made = true;
             if (tid == 0) store_record(a, walk.index, r, w, kFewRows);
