@@ -159,3 +159,18 @@ def test_elements_that_stay_past_31_bits(pairing):
                               (out[r, i:i + (1 << 20), 1], b * c + a * s)):
                 tol = mag + want.abs() * HALF_STEP["bf16"] * (1 + 2 ** -6)
                 assert ((got.double() - want).abs() <= tol).all()
+
+
+def test_a_last_workgroup_of_fewer_rows():
+    """4551 rows, three of them a workgroup's last."""
+    bt = Batch(w=[3] * 41, o=[0] * 41, bl=37, W_max=3).cuda()
+    assert bt.row_cap % 4 == 3
+    for d, sections, pairing in ((32, (5, 4), "halves"), (64, (20,), "neighbours")):
+        freq, axis = fb.rotary_sections(d, sections)
+        q, k, pos = inputs(bt, 2, 1, d, "bf16", len(sections), seed=9)
+        dq, dk = q.cuda(), k.cuda()
+        qo, ko = torch.full_like(dq, 7), torch.full_like(dk, 7)
+        fb.fb_rotary_axes(dq, qo, dk, ko, pos.cuda(), bt.pack, fb.make_shape(2, 1, d, "bf16", 8, 1, 1),
+                          fb.make_rotary(freq, axis, pairing))
+        check(bt, q, qo, pos, freq, axis, pairing, "bf16")
+        check(bt, k, ko, pos, freq, axis, pairing, "bf16")
