@@ -42,7 +42,8 @@ typedef struct fb_rotary {
     int32_t n_pairs;     /* 1 .. head_dim / 2                                  */
     int32_t pairing;     /* FB_PAIR_*                                          */
     int32_t reserved;
-    double  freq[64];    /* finite                                             */
+    double  freq[64];    /* finite; |position * freq| up to 2^53 (angles past
+                            that hold no fraction of a turn)                   */
     uint8_t axis[64];    /* each below n_axes                                  */
 } fb_rotary;
 
@@ -104,6 +105,7 @@ typedef struct fb_mx_cache {
  * same bytes wherever they stand.
  *   k_new, v_new  [row_cap][Hkv][d] (dtype of sh), 16-byte aligned
  *   page_table    int32[B][max_pages]
+ *   bl * Hkv * d/8 at most 2^31 - 2^24
  * A page id outside [0, num_pages) or a position past max_pages*page_size is
  * skipped and recorded as FB_DERR_PAGE. */
 int fb_mx_write_window_kv(const void* k_new, const void* v_new,
@@ -142,6 +144,8 @@ size_t fb_mx_attention_workspace_bytes(const fb_pack* pack, const fb_attn_shape*
  *   q, out  [row_cap][Hq][d] (dtype of sh), 16-byte aligned; out may be q
  *   ws      device workspace of fb_mx_attention_workspace_bytes bytes, 16-byte
  *           aligned
+ * Scores sm_scale * <q, K> are below 2^30 in magnitude (the rows of larger ones may
+ * be NaN), W_max * bl * Hq/Hkv is at most 2^31 - 128.
  * Deterministic: repeated calls give bit-identical results.  How long contexts
  * are divided among workgroups, and so the rounding of a request's rows, goes
  * by the whole pack; kv_split is not read.  A NaN scale spoils the rows that see

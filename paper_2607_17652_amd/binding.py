@@ -658,7 +658,8 @@ def make_rotary(freq, axis, pairing="halves"):
 
 def rotary_sections(head_dim, sections, base=10000.0):
     """(freq, axis) of make_rotary for heads whose first sections[0] pairs turn by axis 0,
-    the next sections[1] by axis 1, and so on, pair j at base^(-2j/head_dim)."""
+    the next sections[1] by axis 1, and so on, pair j at base^(-2j/head_dim).  (A model that
+    turns part of a head may count its frequencies over that width: pass it as head_dim.)"""
     axis = [a for a, n in enumerate(sections) for _ in range(n)]
     return [base ** (-2.0 * j / head_dim) for j in range(len(axis))], axis
 

@@ -21,16 +21,16 @@
 //                    issue of matrix and vector instructions together: 87
 //                    vector instructions (16 of them conversions of codes) to
 //                    16 products, the matrix cores busy 46% of the time.  256
-//                    requests, 20416 rows over 128 .. 8192 keys, 4 bits: 763 us,
-//                    880 TFLOP/s; 8 requests over 16K .. 32K keys, 8 bits: 424
-//                    us, 940 TFLOP/s, which is what the same attention over a
-//                    bf16 cache reaches
+//                    requests, 20416 rows over 128 .. 8192 keys, 4 bits: 757 ..
+//                    827 us over several boxes, 810 .. 890 TFLOP/s; 8 requests
+//                    over 16K .. 32K keys, 8 bits: 421 .. 464 us, 860 .. 950
+//                    TFLOP/s
 //   mx_few_kernel    requests of at most 32 rows (single tokens among them):
 //                    the waves take key tiles in turn, each for all rows, and
 //                    join at the end; no tile is shared, so no wave waits.  Bound
 //                    by memory where the contexts are long: 64 tokens over 1K ..
-//                    32K keys, 639 MB in 4 bits, 140 us, 4.6 TB/s; in 8 bits 1.2
-//                    GB in 245 us, 5.0 TB/s
+//                    32K keys, 639 MB in 4 bits, 141 us, 4.5 TB/s; in 8 bits 1.2
+//                    GB in 236 us, 5.2 TB/s
 //   mx_merge_kernel  the divided units' pieces, by their log-sum-exps (6 .. 15 us)
 //
 // S^T = K Q^T leaves in lane l the scores of query row l % 32 and keys
@@ -56,17 +56,19 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kKeys = 32;              // of a tile
 constexpr int kWideRows = 128, kFewRows = 32;
-// Caches of at most so many keys are walked by one workgroup a unit, with no merge,
-// where there are no more units than workgroups.  Divided and whole: 8 heads, one token,
-// 250 keys 13.4 and 10.9 us, 500 keys 18.2 and 12.6, 1024 keys 18.6 and 17.2; 14 units of
-// 128 rows, 700 keys 19.0 and 16.0, in float32 24.5 and 23.2.
+// Caches that the page table lets hold at most so many keys are walked by one workgroup a
+// unit, with no merge, where there are no more units than workgroups.  Divided and whole: 8
+// heads, one token, 250 keys 11.9 and 10.1 us, 500 keys 16.6 and 12.1, 1024 keys 18.3 and
+// 16.4, 1240 keys 17.7 and 17.2, 1500 keys 18.1 and 18.9.  14 units of 128 rows over heads of
+// 64 in 8 bits: 700 keys 19.6 and 18.9, 960 keys 19.5 and 22.5; in float32, whose crossing
+// lies lower than this bound, 29.3 and 31.3, 29.3 and 38.0.
 constexpr int kWideWholeKeys = 1024, kFewWholeKeys = 1280;
 // what a unit's start and end cost, in tiles: of 128 rows, of 32
-// (256 requests of windows: 4 798 us, 9 777, 14 804; 64 single tokens: 14 154, 20 152, 40 158)
+// (256 requests of windows: 4 780 us, 9 763, 14 782; 64 single tokens: 14 143, 20 142, 40 147)
 constexpr int kWideStart = 9, kFewStart = 20;
 constexpr int kLeastShare = 8;         // of a workgroup, in tiles
 // Workgroups of a CU: as many as their registers let it hold at once.  (Heads of 32 with
-// one fewer: 8 long requests 186 us, 175 so; 64 single tokens in 8 bits 74, 63.5.)
+// one fewer: 8 long requests 188 us, 180 so; 64 single tokens in 8 bits 76, 66.)
 constexpr int per_cu(int D, bool bf16, int rows) {
     return !bf16 ? 2 : rows == kWideRows ? (D == 32 ? 4 : 3) : (D == 32 ? 3 : 2);
 }
@@ -210,9 +212,9 @@ struct Walk {
         }
         share = max(div_of(total + a.wgs - 1, a.wgs), (long long)(kLeastShare + kStart));
         const int busy = (int)div_of(total + share - 1, share);
-        // Neighbours in the line read the same keys, so they belong on one XCD:
-        // workgroups go to the eight in turn (8 long requests: 435 us, 439 without;
-        // 256 requests: 777, 785).
+        // Neighbours in the line read the same keys, so they belong on one XCD: workgroups
+        // go to the eight in turn (8 long requests: 426 us, 429 without; 256 requests: 757,
+        // 758).
         const int each = (busy + 7) / 8;
         index = blockIdx.x % 8 * each + blockIdx.x / 8;
         if (blockIdx.x == 0 && tid == 0) a.head[0] = busy;
@@ -468,9 +470,11 @@ struct Rows {
         }
     }
 
-    // Scores x0 .. x0 + N - 1 into weights.  bf16: they are rounded for the product,
-    // and the denominator sums the rounded ones, so that the rounding cancels where
-    // values agree.
+    // Scores x0 .. x0 + N - 1 into weights.  bf16: they are rounded for the product, as over a
+    // bf16 cache, and the denominator sums the rounded ones, so that the rounding cancels where
+    // values agree.  (Results are off from float64 by 2.1e-3 of their norm over the measured
+    // batches, where their own rounding alone makes 1.66e-3; weights in two parts would be
+    // half as many products again.)
     template <int N>
     __device__ inline void weights(const floatx16& s, int x0, float scale, bf16x8 (&pb)[2][NP]) {
 #pragma unroll
