@@ -174,3 +174,22 @@ def test_a_last_workgroup_of_fewer_rows():
                           fb.make_rotary(freq, axis, pairing))
         check(bt, q, qo, pos, freq, axis, pairing, "bf16")
         check(bt, k, ko, pos, freq, axis, pairing, "bf16")
+
+
+@pytest.mark.parametrize("pairing", ["halves", "neighbours"])
+def test_angles_up_to_2_to_the_53(pairing):
+    """Frequencies up to 2^22 at positions over all of int32.  The count of turns may be off
+    by one, so that the angle that is left, up to 3 pi, is off by 2^-21 as a float32: 8 units
+    of 2^-24; sine and cosine 2 each, two products and a sum."""
+    bt = Batch(**BATCHES["ragged"]).cuda()
+    d, n = 64, 24
+    axis, freq = [j % 3 for j in range(n)], [1.0000001 * 2.0 ** (j - 2) for j in range(n)]
+    q, k, pos = inputs(bt, 4, 4, d, "f32", 3, seed=4, far=True)
+    dq, dk = q.cuda(), k.cuda()
+    qo, ko = torch.full_like(dq, 7), torch.full_like(dk, 7)
+    fb.fb_rotary_axes(dq, qo, dk, ko, pos.cuda(), bt.pack, fb.make_shape(4, 4, d, "f32", 8, 1, 1),
+                      fb.make_rotary(freq, axis, pairing))
+    for x, out in ((q, qo), (k, ko)):
+        want = oc.rotary_axes(f64(x)[bt.live], pos.numpy()[:, bt.live], freq, axis, pairing)
+        mag = np.abs(f64(x)[bt.live]).max() * 2
+        assert np.abs(f64(out)[bt.live] - want).max() <= mag * 20 * EPS
